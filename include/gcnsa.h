@@ -616,6 +616,87 @@ int gcnsa_op_colsum_scaled(void* stream, int64_t n, int32_t f, const float* g, i
 int gcnsa_op_colsum_static(void* stream, int64_t n, int32_t f, const float* g, int64_t ldg, float* out,
                            int32_t accumulate);
 
+/* ---- layer norm, 8-bit checkpoints of activations, output layers of many classes ----
+ *
+ * For models beyond the paper's two layers (it stacks up to a few, Section 4.1):
+ * a norm between layers, hidden rows kept in 8 bits until the backward pass, and
+ * a loss whose logits are never stored.  Results whose leading dimension leaves
+ * room have zeros in the pad columns up to the next multiple of 4. */
+
+/* A checkpoint of n rows of f columns.  Every 32 columns of a row share a step
+ * 2^(e - 127); a value is q * step, q in [-127, 127].  e is the smallest byte
+ * from 1 on with which the largest magnitude of the 32 rounds to at most 127
+ * steps, so that no value is off by more than half a step (ties to even; e ends
+ * at 248, and magnitudes from 127.5 2^121 on are kept as 127 2^121).  32
+ * columns with an infinity or a NaN among them get e = 255 and are restored as
+ * NaN.  The struct is HOST memory, its pointers are DEVICE. */
+typedef struct {
+  int8_t* q;   /* [n x ldq] 16-byte aligned; columns up to the next multiple of 16 are written (zeros) */
+  int64_t ldq; /* a multiple of 16, at least f                                                       */
+  uint8_t* e;  /* [n x lde]                                                                          */
+  int64_t lde; /* at least ceil(f / 32)                                                              */
+} gcnsa_packed8;
+
+/* Layer norm of every row: y = (x - mean) rstd gamma + beta, rstd = 1 / sqrt(var
+ * + eps), var the mean of (x - mean)^2; relu != 0: then max(y, 0) (a NaN stays
+ * one).  gamma, beta: nullable DEVICE [f] (1 and 0); mean, rstd: nullable DEVICE
+ * [n], what gcnsa_op_layer_norm_backward needs; x8, y8: nullable, receive
+ * checkpoints of x and of y in the same pass; bits: nullable DEVICE [n x ldbits],
+ * ldbits >= ceil(f / 32), with relu only: bit j % 32 of word j / 32 of a row says
+ * whether the ReLU let value j through.  y may be x (same ld).  1 <= f <=
+ * GCNSA_NORM_MAX_F, eps > 0. */
+#define GCNSA_NORM_MAX_F (1 << 24)
+int gcnsa_op_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const float* gamma,
+                        const float* beta, float eps, int32_t relu, float* y, int64_t ldy, float* mean, float* rstd,
+                        const gcnsa_packed8* x8, const gcnsa_packed8* y8, uint32_t* bits, int64_t ldbits);
+/* Its backward pass from the gradient g w.r.t. y: with xh = (x - mean) rstd and
+ * u = g gamma (0 where relu != 0 and xh gamma + beta is not above 0, or, with the
+ * forward pass's bits given, where these say so: the half steps of a checkpoint
+ * turn the sign of about 1 value in 400, which alone puts a gradient 7 % off),
+ * dx = rstd (u - mean(u) - xh mean(u xh)); dgamma[j] (+)= sum_i g[i, j] xh[i, j] and
+ * dbeta[j] (+)= sum_i g[i, j] over the gradients the ReLU let through.  The input
+ * is either x or its checkpoint x8 (the other one NULL).  mean, rstd: DEVICE [n],
+ * from the forward pass; gamma, beta, dgamma, dbeta nullable; dx may be g or x
+ * (same ld).  scratch: DEVICE, gcnsa_op_layer_norm_backward_scratch(n, f) bytes,
+ * not needed (NULL) without dgamma and dbeta.  Sums are added in a fixed order. */
+int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float* g, int64_t ldg, const float* x,
+                                 int64_t ldx, const gcnsa_packed8* x8, const float* mean, const float* rstd,
+                                 const float* gamma, const float* beta, int32_t relu, const uint32_t* bits,
+                                 int64_t ldbits, float* dx, int64_t lddx, float* dgamma, float* dbeta,
+                                 int32_t accumulate, void* scratch, size_t scratch_bytes);
+size_t gcnsa_op_layer_norm_backward_scratch(int64_t n, int32_t f);
+
+/* Make a checkpoint of x, and restore one. */
+int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p);
+int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx);
+
+/* dw (+)= X^T G with X [n x f] a checkpoint and G [n x c]: the weight gradient of a
+ * layer whose input was kept in 8 bits.  fp32-level accuracy with respect to the
+ * values the checkpoint stands for.  n, f, c < 2^31; workspace: DEVICE, 256-byte
+ * aligned, gcnsa_op_gemm_packed8_workspace(n, f, c) bytes (NULL when that is 0). */
+int gcnsa_op_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g,
+                          int64_t ldg, float* dw, int64_t lddw, int32_t accumulate, void* workspace,
+                          size_t workspace_bytes);
+size_t gcnsa_op_gemm_packed8_workspace(int64_t n, int32_t f, int32_t c);
+
+/* Masked softmax cross-entropy of an output layer, loss and gradients in one call:
+ * z = h w + bias [n x c], *loss = (1/n_train) sum over masked rows of
+ * (logsumexp(z_i) - z_i[y_i]), G = (softmax - onehot) mask / n_train, dh = G w^T,
+ * dw (+)= h^T G, db (+)= column sums of G.  z and G only ever exist for a piece of
+ * the classes at a time, in the workspace.  h [n x d], w [d x c], dh [n x d], dw
+ * [d x c], db [c], y [n], mask [n] (NULL: every row), loss: DEVICE; bias, dh, dw,
+ * db nullable (what is not asked for is not computed).  n_train is the number of
+ * masked rows (n without a mask); with another number the loss comes out as NaN.
+ * n_train = 0: loss 0, zero gradients.  Labels of masked rows lie in [0, c); one
+ * that does not makes the loss NaN (nothing is read or written out of place).
+ * accumulate applies to dw and db.  d, c >= 1; n, d, c < 2^31; workspace: DEVICE,
+ * 256-byte aligned, gcnsa_op_linear_ce_workspace(n, d, c) bytes. */
+int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const float* h, int64_t ldh, const float* w,
+                       int64_t ldw, const float* bias, const int32_t* y, const uint8_t* mask, int64_t n_train,
+                       float* loss, float* dh, int64_t lddh, float* dw, int64_t lddw, float* db, int32_t accumulate,
+                       void* workspace, size_t workspace_bytes);
+size_t gcnsa_op_linear_ce_workspace(int64_t n, int32_t d, int32_t c);
+
 /* g = gsum * inv_m; Adam step number t (>= 1) on theta with moments m, v; gsum
  * cleared.  All DEVICE [count]. */
 int gcnsa_op_adam(void* stream, int64_t count, float* theta, float* gsum, float* m, float* v, float inv_m,

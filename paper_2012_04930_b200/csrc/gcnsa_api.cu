@@ -1607,6 +1607,116 @@ int gcnsa_op_colsum_scaled(void* stream, int64_t n, int32_t f, const float* g, i
   return GCNSA_OK;
 }
 
+// NULL when the checkpoint can be used, else what is wrong with it
+static const char* packed_fault(const gcnsa_packed8* p, int32_t f) {
+  if (!p->q || !p->e) return "NULL pointer in a checkpoint";
+  if (p->ldq % 16 || p->ldq < f || !aligned16(p->q)) return "a checkpoint needs a 16-byte aligned base and a leading dimension that is a multiple of 16 and at least f";
+  if (p->lde < ((int64_t)f + 31) / 32) return "a checkpoint has a step for every 32 columns";
+  return nullptr;
+}
+
+int gcnsa_op_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const float* gamma, const float* beta,
+                        float eps, int32_t relu, float* y, int64_t ldy, float* mean, float* rstd, const gcnsa_packed8* x8,
+                        const gcnsa_packed8* y8, uint32_t* bits, int64_t ldbits) {
+  if (n < 0 || f < 1) return fail(GCNSA_ERR_ARG, "negative dimension or f < 1");
+  if (f > GCNSA_NORM_MAX_F) return fail(GCNSA_ERR_TOO_LARGE, "f exceeds GCNSA_NORM_MAX_F");
+  if (!(eps > 0.f) || std::isinf(eps)) return fail(GCNSA_ERR_ARG, "eps must be positive and finite");
+  if (ldx < f || ldy < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");
+  for (const gcnsa_packed8* p : {x8, y8})
+    if (const char* what = p && n > 0 ? packed_fault(p, f) : nullptr) return fail(GCNSA_ERR_ARG, what);
+  if (bits && (!relu || ldbits < ((int64_t)f + 31) / 32)) return fail(GCNSA_ERR_ARG, "bits go with relu, a word for every 32 columns");
+  if (n == 0) return GCNSA_OK;
+  if (!x || !y) return fail(GCNSA_ERR_ARG, "NULL pointer");
+  if (x == y && ldx != ldy) return fail(GCNSA_ERR_ARG, "in place needs one leading dimension");
+  CKL(launch_layer_norm(stream, n, f, x, ldx, gamma, beta, eps, relu, y, ldy, mean, rstd, x8, y8, bits, ldbits));
+  return GCNSA_OK;
+}
+
+size_t gcnsa_op_layer_norm_backward_scratch(int64_t n, int32_t f) { return layer_norm_grad_scratch(n < 0 ? 0 : n, f < 0 ? 0 : f); }
+
+int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float* g, int64_t ldg, const float* x, int64_t ldx,
+                                 const gcnsa_packed8* x8, const float* mean, const float* rstd, const float* gamma,
+                                 const float* beta, int32_t relu, const uint32_t* bits, int64_t ldbits, float* dx, int64_t lddx,
+                                 float* dgamma, float* dbeta, int32_t accumulate, void* scratch, size_t scratch_bytes) {
+  if (n < 0 || f < 1) return fail(GCNSA_ERR_ARG, "negative dimension or f < 1");
+  if (f > GCNSA_NORM_MAX_F) return fail(GCNSA_ERR_TOO_LARGE, "f exceeds GCNSA_NORM_MAX_F");
+  if (bits && (!relu || ldbits < ((int64_t)f + 31) / 32)) return fail(GCNSA_ERR_ARG, "bits go with relu, a word for every 32 columns");
+  if ((dgamma || dbeta) && (!scratch || ((uintptr_t)scratch & 3) || scratch_bytes < layer_norm_grad_scratch(n, f)))
+    return fail(GCNSA_ERR_ARG, "scratch missing, unaligned or too small");
+  if (n > 0) {
+    if (!g || !dx || !mean || !rstd) return fail(GCNSA_ERR_ARG, "NULL pointer");
+    if (!x == !x8) return fail(GCNSA_ERR_ARG, "either x or its checkpoint");
+    if (ldg < f || lddx < f || (x && ldx < f)) return fail(GCNSA_ERR_ARG, "leading dimension too small");
+    if ((dx == g && lddx != ldg) || (dx == x && lddx != ldx)) return fail(GCNSA_ERR_ARG, "in place needs one leading dimension");
+    if (const char* what = x8 ? packed_fault(x8, f) : nullptr) return fail(GCNSA_ERR_ARG, what);
+  }
+  CKL(launch_layer_norm_grad(stream, n, f, g, ldg, x, ldx, x8, mean, rstd, gamma, beta, relu, bits, ldbits, dx, lddx, dgamma,
+                             dbeta, accumulate, scratch));
+  return GCNSA_OK;
+}
+
+int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p) {
+  if (n < 0 || f < 1) return fail(GCNSA_ERR_ARG, "negative dimension or f < 1");
+  if (n == 0) return GCNSA_OK;
+  if (!x || !p) return fail(GCNSA_ERR_ARG, "NULL pointer");
+  if (ldx < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");
+  if (const char* what = packed_fault(p, f)) return fail(GCNSA_ERR_ARG, what);
+  CKL(launch_pack8(stream, n, f, x, ldx, p));
+  return GCNSA_OK;
+}
+
+int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx) {
+  if (n < 0 || f < 1) return fail(GCNSA_ERR_ARG, "negative dimension or f < 1");
+  if (n == 0) return GCNSA_OK;
+  if (!x || !p) return fail(GCNSA_ERR_ARG, "NULL pointer");
+  if (ldx < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");
+  if (const char* what = packed_fault(p, f)) return fail(GCNSA_ERR_ARG, what);
+  CKL(launch_unpack8(stream, n, f, p, x, ldx));
+  return GCNSA_OK;
+}
+
+static bool workspace_ok(const void* w, size_t bytes, size_t need) { return need == 0 || (w && ((uintptr_t)w & 255) == 0 && bytes >= need); }
+
+size_t gcnsa_op_gemm_packed8_workspace(int64_t n, int32_t f, int32_t c) {
+  return n <= 0 || f <= 0 || c <= 0 ? 0 : gemm_packed8_workspace(n, f, c);
+}
+
+int gcnsa_op_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g, int64_t ldg,
+                          float* dw, int64_t lddw, int32_t accumulate, void* workspace, size_t workspace_bytes) {
+  if (n < 0 || f < 0 || c < 0 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension");
+  if (f == 0 || c == 0) return GCNSA_OK;
+  if (!dw || (n > 0 && (!x || !g))) return fail(GCNSA_ERR_ARG, "NULL pointer");
+  if (lddw < c || (n > 0 && ldg < c)) return fail(GCNSA_ERR_ARG, "leading dimension too small");
+  if (const char* what = n > 0 ? packed_fault(x, f) : nullptr) return fail(GCNSA_ERR_ARG, what);
+  if (!workspace_ok(workspace, workspace_bytes, gcnsa_op_gemm_packed8_workspace(n, f, c)))
+    return fail(GCNSA_ERR_ARG, "workspace missing, unaligned or too small");
+  CKL(launch_gemm_packed8(stream, n, f, c, x, g, ldg, dw, lddw, accumulate, workspace));
+  return GCNSA_OK;
+}
+
+size_t gcnsa_op_linear_ce_workspace(int64_t n, int32_t d, int32_t c) {
+  return d < 1 || c < 1 ? 0 : linear_ce_workspace(n < 0 ? 0 : n, d, c);
+}
+
+int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const float* h, int64_t ldh, const float* w, int64_t ldw,
+                       const float* bias, const int32_t* y, const uint8_t* mask, int64_t n_train, float* loss, float* dh,
+                       int64_t lddh, float* dw, int64_t lddw, float* db, int32_t accumulate, void* workspace,
+                       size_t workspace_bytes) {
+  if (n < 0 || d < 1 || c < 1 || n_train < 0 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension, d < 1 or c < 1");
+  if (n_train > n || (!mask && n_train != n)) return fail(GCNSA_ERR_ARG, "n_train is the number of masked rows");
+  if (!loss || !w || (n > 0 && (!h || !y))) return fail(GCNSA_ERR_ARG, "NULL pointer");
+  if (ldw < c || (dw && lddw < c) || (n > 0 && (ldh < d || (dh && lddh < d)))) return fail(GCNSA_ERR_ARG, "leading dimension too small");
+  if ((n > 0 && dh == h) || dw == w) return fail(GCNSA_ERR_ARG, "dh and dw must not be h and w");
+  if (!workspace_ok(workspace, workspace_bytes, linear_ce_workspace(n, d, c)))
+    return fail(GCNSA_ERR_ARG, "workspace missing, unaligned or too small");
+  LinearCe a;
+  a.n = n; a.n_train = n_train; a.d = d; a.c = c; a.accumulate = accumulate;
+  a.h = h; a.ldh = ldh; a.w = w; a.ldw = ldw; a.bias = bias; a.y = y; a.mask = mask;
+  a.loss = loss; a.dh = dh; a.lddh = lddh; a.dw = dw; a.lddw = lddw; a.db = db;
+  CKL(launch_linear_ce(stream, a, workspace));
+  return GCNSA_OK;
+}
+
 int gcnsa_op_adam(void* stream, int64_t count, float* theta, float* gsum, float* m, float* v, float inv_m, float lr,
                   float beta1, float beta2, float eps, int64_t t) {
   if (count < 0 || t < 1) return fail(GCNSA_ERR_ARG, "negative count or t < 1");

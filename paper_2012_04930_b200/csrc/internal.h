@@ -300,4 +300,32 @@ int launch_scale_rows(void* stream, int64_t n, int32_t f, const float* scale, co
                       int64_t ldd);
 int launch_mean(void* stream, const float* src, int count, float* dst);  // dst[0] = mean(src[0..count))
 
+
+// ---- layer norm, 8-bit checkpoints (kernels_norm.cu), products with them and the loss of an output layer ----
+int launch_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const float* gamma, const float* beta,
+                      float eps, int32_t relu, float* y, int64_t ldy, float* mean, float* rstd, const gcnsa_packed8* x8,
+                      const gcnsa_packed8* y8, uint32_t* bits, int64_t ldbits);
+int launch_layer_norm_grad(void* stream, int64_t n, int32_t f, const float* g, int64_t ldg, const float* x, int64_t ldx,
+                           const gcnsa_packed8* x8, const float* mean, const float* rstd, const float* gamma, const float* beta,
+                           int32_t relu, const uint32_t* bits, int64_t ldbits, float* dx, int64_t lddx, float* dgamma, float* dbeta,
+                           int32_t accumulate, void* scratch);
+size_t layer_norm_grad_scratch(int64_t n, int32_t f);
+int launch_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p);
+int launch_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx);
+int launch_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g, int64_t ldg,
+                        float* dw, int64_t lddw, int32_t accumulate, void* workspace);
+size_t gemm_packed8_workspace(int64_t n, int32_t f, int32_t c);
+struct LinearCe {
+  int64_t n = 0, n_train = 0;
+  int32_t d = 0, c = 0, accumulate = 0;
+  const float *h = nullptr, *w = nullptr, *bias = nullptr;
+  int64_t ldh = 0, ldw = 0;
+  const int32_t* y = nullptr;
+  const uint8_t* mask = nullptr;
+  float *loss = nullptr, *dh = nullptr, *dw = nullptr, *db = nullptr;
+  int64_t lddh = 0, lddw = 0;
+};
+int launch_linear_ce(void* stream, const LinearCe& a, void* workspace);
+size_t linear_ce_workspace(int64_t n, int32_t d, int32_t c);
+
 }  // namespace gcnsa

@@ -90,6 +90,10 @@ class Profile(C.Structure):
                 ("flops", C.c_double * 3), ("l1_bytes", C.c_double * 3), ("alg_bytes_val", C.c_double * 3)]
 
 
+class Packed8Dev(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ldq", C.c_int64), ("e", C.c_void_p), ("lde", C.c_int64)]
+
+
 class GcnsaError(RuntimeError):
     def __init__(self, code, text):
         super().__init__(f"gcnsa error {code}: {text}")
@@ -180,6 +184,23 @@ _SIGS = {
     "gcnsa_op_colsum_scaled": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32,
                                          C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_int64]),
     "gcnsa_op_colsum_static": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32]),
+    "gcnsa_op_layer_norm": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float,
+                                      C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.POINTER(Packed8Dev),
+                                      C.POINTER(Packed8Dev), C.c_void_p, C.c_int64]),
+    "gcnsa_op_layer_norm_backward": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                               C.POINTER(Packed8Dev), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                               C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                               C.c_int32, C.c_void_p, C.c_size_t]),
+    "gcnsa_op_layer_norm_backward_scratch": (C.c_size_t, [C.c_int64, C.c_int32]),
+    "gcnsa_op_pack8": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.POINTER(Packed8Dev)]),
+    "gcnsa_op_unpack8": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.POINTER(Packed8Dev), C.c_void_p, C.c_int64]),
+    "gcnsa_op_gemm_packed8": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.POINTER(Packed8Dev), C.c_void_p,
+                                        C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_size_t]),
+    "gcnsa_op_gemm_packed8_workspace": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
+    "gcnsa_op_linear_ce": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                     C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t]),
+    "gcnsa_op_linear_ce_workspace": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
     "gcnsa_op_adam": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                 C.c_float, C.c_float, C.c_float, C.c_float, C.c_int64]),
     "gcnsa_op_normalize": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -723,6 +744,154 @@ COLSUM_STATIC_MAX_F = 1024
 
 def op_colsum_scratch(n, f) -> int:
     return int(lib().gcnsa_op_colsum_scratch(n, f))
+
+
+# ---- layer norm, 8-bit checkpoints, output layers: operands are checked here, as a host pointer or another device's would
+# fault on the GPU ----
+def _refuse(what):
+    raise GcnsaError(ERR_ARG, what)
+
+
+def _operand(t, name, dtype, rows=None, cols=None, like=None):
+    """(pointer, leading dimension) of a device tensor: [rows x >= cols] with contiguous columns, or (cols None) a contiguous
+    vector of at least `rows` elements."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or (like is not None and t.device != like.device):
+        _refuse(f"{name}: on {t.device}, expected {'a CUDA device' if like is None else like.device}")
+    if str(t.dtype) != "torch." + dtype:
+        _refuse(f"{name}: {t.dtype}, expected {dtype}")
+    if cols is None:
+        if t.numel() < (rows or 0) or not t.is_contiguous():
+            _refuse(f"{name}: a contiguous vector of {rows} elements is needed, got {tuple(t.shape)}")
+        return _dp(t), 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"{name}: rows of contiguous columns are needed, [{rows} x at least {cols}], got {tuple(t.shape)} with strides {t.stride()}")
+    # (the stride of a single row says nothing)
+    return _dp(t), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], cols)
+
+
+def _on(t):
+    """The stream that a call on t's device goes to; that device has to be the current one."""
+    import torch
+    if t.device.index != torch.cuda.current_device():
+        _refuse(f"tensors on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream()
+
+
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _rows_of(t, name):
+    if t is None or t.dim() != 2:
+        _refuse(f"{name}: a matrix is needed")
+    return t.shape[0]
+
+
+class Packed8:
+    """An 8-bit checkpoint of n rows of f columns: q (int8 [n x a multiple of 16]) and e (uint8 [n x ceil(f / 32)], the biased
+    exponents of the steps); makes its own tensors unless given."""
+
+    def __init__(self, n, f, q=None, e=None, device=None):
+        import torch
+        if n < 0 or f < 1:
+            _refuse(f"a checkpoint of {n} x {f}")
+        self.n, self.f = int(n), int(f)
+        dev = device if device is not None else "cuda"
+        self.q = torch.zeros((n, (f + 15) // 16 * 16), dtype=torch.int8, device=dev) if q is None else q
+        self.e = torch.zeros((n, (f + 31) // 32), dtype=torch.uint8, device=dev) if e is None else e
+
+    def dev(self, name="checkpoint", n=None, f=None, like=None) -> Packed8Dev:
+        if (n is not None and n != self.n) or (f is not None and f != self.f):
+            _refuse(f"{name}: {self.n} x {self.f}, expected {n} x {f}")
+        q, ldq = _operand(self.q, name + ".q", "int8", self.n, (self.f + 15) // 16 * 16, like)
+        e, lde = _operand(self.e, name + ".e", "uint8", self.n, (self.f + 31) // 32, self.q)
+        return Packed8Dev(q=q, ldq=ldq, e=e, lde=lde)
+
+
+def _packed(p, name, n, f, like):
+    return None if p is None else C.byref(p.dev(name, n, f, like))
+
+
+def op_layer_norm(x, f, y, gamma=None, beta=None, eps=1e-5, relu=0, mean=None, rstd=None, x8=None, y8=None, bits=None):
+    """y = norm of the rows of x (first f columns), then gamma, beta and (relu) ReLU; mean and rstd per row are what the
+    backward pass needs; x8 and y8 (Packed8) receive checkpoints of x and of y, bits (int32 [n x ceil(f / 32)]) what the ReLU
+    let through."""
+    n = _rows_of(x, "x")
+    xp, ldx = _operand(x, "x", "float32", n, f)
+    yp, ldy = _operand(y, "y", "float32", n, f, x)
+    vec = [_operand(t, nm, "float32", k, None, x)[0] for t, nm, k in ((gamma, "gamma", f), (beta, "beta", f), (mean, "mean", n), (rstd, "rstd", n))]
+    _ck(lib().gcnsa_op_layer_norm(_on(x), n, f, xp, ldx, vec[0], vec[1], eps, int(relu), yp, ldy, vec[2], vec[3],
+                                  _packed(x8, "x8", n, f, x), _packed(y8, "y8", n, f, x),
+                                  *_operand(bits, "bits", "int32", n, (f + 31) // 32, x)))
+
+
+def op_layer_norm_backward(g, x, f, dx, mean, rstd, gamma=None, beta=None, relu=0, dgamma=None, dbeta=None, accumulate=0,
+                           scratch=None, bits=None):
+    """dx (and dgamma, dbeta) of op_layer_norm from the gradient g w.r.t. its result; x is its input or a Packed8 of it, bits
+    what the forward pass said of the ReLU (without: taken from x)."""
+    n = _rows_of(g, "g")
+    gp, ldg = _operand(g, "g", "float32", n, f)
+    dxp, lddx = _operand(dx, "dx", "float32", n, f, g)
+    x8 = _packed(x, "x", n, f, g) if isinstance(x, Packed8) else None
+    xp, ldx = (None, 0) if x8 is not None else _operand(x, "x", "float32", n, f, g)
+    vec = [_operand(t, nm, "float32", k, None, g)[0] for t, nm, k in
+           ((mean, "mean", n), (rstd, "rstd", n), (gamma, "gamma", f), (beta, "beta", f), (dgamma, "dgamma", f), (dbeta, "dbeta", f))]
+    if scratch is not None:
+        _operand(scratch, "scratch", str(scratch.dtype)[6:], 0, None, g)
+    _ck(lib().gcnsa_op_layer_norm_backward(_on(g), n, f, gp, ldg, xp, ldx, x8, vec[0], vec[1], vec[2], vec[3], int(relu),
+                                           *_operand(bits, "bits", "int32", n, (f + 31) // 32, g), dxp, lddx, vec[4], vec[5], accumulate, _dp(scratch), _nbytes(scratch)))
+
+
+def op_layer_norm_backward_scratch(n, f) -> int:
+    return int(lib().gcnsa_op_layer_norm_backward_scratch(n, f))
+
+
+def op_pack8(x, p):
+    """Checkpoint of the first p.f columns of x."""
+    xp, ldx = _operand(x, "x", "float32", p.n, p.f)
+    _ck(lib().gcnsa_op_pack8(_on(x), p.n, p.f, xp, ldx, _packed(p, "p", None, None, x)))
+
+
+def op_unpack8(p, x):
+    """x = what the checkpoint stands for (first p.f columns)."""
+    xp, ldx = _operand(x, "x", "float32", p.n, p.f)
+    _ck(lib().gcnsa_op_unpack8(_on(x), p.n, p.f, _packed(p, "p", None, None, x), xp, ldx))
+
+
+def op_gemm_packed8(p, g, c, dw, accumulate=0, workspace=None):
+    """dw (+)= X^T G with X a checkpoint [n x f] and G the first c columns of g."""
+    gp, ldg = _operand(g, "g", "float32", p.n, c)
+    dwp, lddw = _operand(dw, "dw", "float32", p.f, c, g)
+    if workspace is not None:
+        _operand(workspace, "workspace", str(workspace.dtype)[6:], 0, None, g)
+    _ck(lib().gcnsa_op_gemm_packed8(_on(g), p.n, p.f, c, _packed(p, "p", None, None, g), gp, ldg, dwp, lddw, accumulate,
+                                    _dp(workspace), _nbytes(workspace)))
+
+
+def op_gemm_packed8_workspace(n, f, c) -> int:
+    return int(lib().gcnsa_op_gemm_packed8_workspace(n, f, c))
+
+
+def op_linear_ce(h, d, w, c, y, n_train, loss, dh=None, dw=None, db=None, bias=None, mask=None, accumulate=0, workspace=None):
+    """Loss of the output layer z = h w + bias under masked softmax cross-entropy, and the gradients asked for (see
+    include/gcnsa.h); n_train is the number of masked rows."""
+    n = _rows_of(h, "h")
+    hp, ldh = _operand(h, "h", "float32", n, d)
+    wp, ldw = _operand(w, "w", "float32", d, c, h)
+    dhp, lddh = _operand(dh, "dh", "float32", n, d, h)
+    dwp, lddw = _operand(dw, "dw", "float32", d, c, h)
+    yp, mp = _operand(y, "y", "int32", n, None, h)[0], _operand(mask, "mask", "uint8", n, None, h)[0]
+    vec = [_operand(t, nm, "float32", k, None, h)[0] for t, nm, k in ((bias, "bias", c), (loss, "loss", 1), (db, "db", c))]
+    if workspace is not None:
+        _operand(workspace, "workspace", str(workspace.dtype)[6:], 0, None, h)
+    _ck(lib().gcnsa_op_linear_ce(_on(h), n, d, c, hp, ldh, wp, ldw, vec[0], yp, mp, n_train, vec[1], dhp, lddh, dwp, lddw, vec[2],
+                                 accumulate, _dp(workspace), _nbytes(workspace)))
+
+
+def op_linear_ce_workspace(n, d, c) -> int:
+    return int(lib().gcnsa_op_linear_ce_workspace(n, d, c))
 
 
 def op_adam(theta, gsum, m, v, inv_m, lr, beta1, beta2, eps, t):
