@@ -541,7 +541,8 @@ int gcnsa_op_gather_probe_warps(int32_t* warps_out);
 
 /* The tensor-core kernels bound every wait (tens of milliseconds); a wait that
  * runs out stores a non-zero code in a device word instead of hanging.  The
- * word (one for the dense products, one for the planned sparse ones) is sticky:
+ * word (one for the dense products, one for the planned sparse ones, one for the
+ * products with checkpoints and of wide output layers) is sticky:
  * while it is set, every launch of its kind returns at once without computing,
  * so results after a non-zero status are undefined until
  * gcnsa_tc_clear.  gcnsa_tc_status synchronizes the device and copies the word

@@ -245,6 +245,8 @@ int tc_status(int* out);  // error word of the tensor-core kernels (0 = no wait 
 int tc_clear();           // sets that word back to 0
 int tc_status_gemm(int* out);  // the dense products' share of it
 int tc_clear_gemm();
+int tc_status_head(int* out);  // and that of the products in kernels_head.cu
+int tc_clear_head();
 // What the softmax kernel can write beside the gradient while that is in registers; rows on 16-byte boundaries only.
 struct CeSide {
   const float* row_scale = nullptr;

@@ -38,6 +38,7 @@
 #include "internal.h"
 #include "launch.h"
 #include "tc_device.h"
+#include "tma_host.h"
 
 namespace gcnsa {
 
@@ -845,23 +846,6 @@ gemm_tf32x3(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiledFn)p;
-  });
-  return fn;
-}
-
 // fp32 matrix with `inner` contiguous elements per line and `outer` lines, pitch ld floats; box = 32 x box_outer,
 // zero fill outside.  K-major operand: inner = k, outer = rows, box_outer = tile rows, 128-byte swizzle.
 // MN-major operand: inner = rows (M or N), outer = k, box_outer = 32; B with the 128-byte swizzle of 32-byte atoms
@@ -888,17 +872,6 @@ struct TcPlan {
 
 // products that run side by side are cut by the rule below up to this many k-blocks
 constexpr int kBesideBlocks = 256;
-
-int sm_count() {
-  static int n = 0;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
-      n = 148;
-  });
-  return n;
-}
 
 // How many clusters of that many blocks (an SM each) run at the same time.  A cluster lives in one of the chip's parts, whose
 // numbers of SMs differ: 16 tiles of eight slices (2 048 x 128 x 2 080) are two rounds and take 24.6 us, 15.1 as single blocks.

@@ -1,12 +1,22 @@
 // The weight gradient of a layer whose input is an 8-bit checkpoint, and the softmax cross-entropy of an output layer
-// over many classes without its logits.
+// over many classes without its logits.  Both are products of kernels_terms.h.
+//
+// Output layer: z = H W + b, G = (softmax(z) - onehot) / n_train, dH = G W^T, dW = H^T G, db = 1^T G.  z is made tile by
+// tile and never leaves the SM; G is written transposed (thread = row, so a class is a line of memory), which is how both
+// gradient products want it: dH^T = W G^T and dW^T = G^T H have a K-major left and an MN-major right operand, and their
+// results, written transposed, are dH and dW.  db falls out of the second one, whose left operand passes through registers.
+//  - c <= 128: a tile holds whole rows of z, so softmax, loss and G come from one pass over the products.
+//  - c > 128: one pass keeps a running maximum and sum of exponentials per row (8 bytes per row and run of tiles), then, a
+//    piece of the classes at a time, z is made again and turned into G.  A piece is as large as keeps G^T in L2.  Rows that
+//    do not count are left out of all products: the others are gathered first.
+// The two gradient products of a piece are independent and run as one launch, the slices of dW^T before the tiles of dH^T.
 #include <cuda_runtime.h>
 
 #include <algorithm>
 
 #include "internal.h"
+#include "kernels_terms.h"
 #include "launch.h"
-#include "pack8_device.h"
 
 namespace gcnsa {
 
@@ -14,200 +24,475 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+int64_t up4(int64_t n) { return (n + 3) / 4 * 4; }
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// ---- dw = X^T G, X packed: 32 x 32 tiles of dw, a slice of the rows per block ---------------------------------------
-constexpr int kTile = 32;
-__global__ void __launch_bounds__(256)
-packed8_product(int64_t n, int f, int c, gcnsa_packed8 x, const float* __restrict__ g, int64_t ldg, int64_t rows_per_slice,
-                float* __restrict__ partial, int64_t ldp) {
-  wait_for_predecessors();
-  __shared__ float xs[kTile][kTile + 1], gs[kTile][kTile + 1];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int f0 = blockIdx.x * kTile, c0 = blockIdx.y * kTile;
-  const int64_t r0 = (int64_t)blockIdx.z * rows_per_slice, r1 = min(n, r0 + rows_per_slice);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t r = r0; r < r1; r += kTile) {
-    for (int k = ty; k < kTile; k += 8) {
-      const int64_t row = r + k;
-      xs[k][tx] = row < r1 && f0 + tx < f ? (float)x.q[row * x.ldq + f0 + tx] * pack8_step(x.e[row * x.lde + f0 / kPackBlock]) : 0.f;
-      gs[k][tx] = row < r1 && c0 + tx < c ? g[row * ldg + c0 + tx] : 0.f;
+// Slices of the inner dimension: as many as make the rounds of tiles x slices items over the SMs shortest, a slice costing
+// about six k-blocks on top of its own (its share of the sums written and read again, an accumulator's start and end).
+int pick_slices(int64_t tiles, int64_t units) {
+  const int64_t sms = sm_count();
+  int64_t best = 1, best_cost = INT64_MAX;
+  for (int64_t s = 1; s <= std::min<int64_t>(units, std::max<int64_t>(1, 2 * sms / tiles)); ++s) {
+    const int64_t cost = div_up(tiles * s, sms) * (div_up(units, s) + 6);
+    if (cost < best_cost) {
+      best = s;
+      best_cost = cost;
     }
-    __syncthreads();
-#pragma unroll 8
-    for (int k = 0; k < kTile; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = fmaf(xs[k][ty + 8 * i], gs[k][tx], acc[i]);
-    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (f0 + ty + 8 * i < f && c0 + tx < c) partial[((int64_t)blockIdx.z * f + f0 + ty + 8 * i) * ldp + c0 + tx] = acc[i];
+  return (int)div_up(units, div_up(units, best));
 }
-int packed8_slices(int64_t n, int32_t f, int32_t c) {
-  const int64_t tiles = (((int64_t)f + kTile - 1) / kTile) * (((int64_t)c + kTile - 1) / kTile);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(n + 255) / 256, 148 * 8 / tiles, 1024}));
+void set_slices(Product& p, int bn, int slices) {
+  p.tiles_m = (int)div_up(p.M, BM);
+  p.tiles_n = (int)div_up(p.N, bn);
+  p.per_slice = (int)div_up(p.units, slices);
+  p.items = p.tiles_m * p.tiles_n * slices;
 }
 
-// ---- softmax cross-entropy over pieces of the classes: z of a piece is in memory, rows carry their running maximum and
-// sum of exponentials (m, s) and their label's logit ------------------------------------------------------------------
-struct RowState {
-  float *m, *s, *zy;
+// ---- dw = X^T G: dw^T = G^T X, tiles of 128 columns of G x 64 or 128 features --------------------------------------
+struct PackedPlan {
+  int bn, slices;
+  int64_t ldp;
 };
-__global__ void __launch_bounds__(256)
-ce_piece_stats(int64_t n, int c0, int width, const float* __restrict__ z, int64_t ldz, const int32_t* __restrict__ y, RowState st) {
+PackedPlan packed_plan(int64_t n, int32_t f, int32_t c) {
+  PackedPlan p;
+  p.bn = f <= 64 ? 64 : 128;
+  p.slices = pick_slices(div_up(c, BM) * div_up(f, p.bn), div_up(n, BK));
+  p.ldp = up4(c);
+  return p;
+}
+template <int BN, ASrc A>
+cudaError_t run_packed(cudaStream_t s, const TermArgs& a, int grid) {
+  return run_terms<TermShape<BN, A, true, Out::transposed>>(s, a, grid);
+}
+
+// ---- rows that count ---------------------------------------------------------------------------------------------------
+constexpr int kRowsPerBlock = 1024;
+__global__ void __launch_bounds__(kRowsPerBlock) mask_counts(int64_t n, const uint8_t* __restrict__ mask, int* __restrict__ counts) {
   wait_for_predecessors();
-  const int lane = threadIdx.x & 31;
-  for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += (int64_t)gridDim.x * 8) {
-    const float* r = z + row * ldz;
-    float m = -INFINITY;
-    for (int j = lane; j < width; j += 32) m = fmaxf(m, r[j]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
-    float s = 0.f;
-    for (int j = lane; j < width; j += 32) s += expf(r[j] - m);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-    if (lane == 0) {
-      if (c0 > 0) {
-        const float m0 = st.m[row], m1 = fmaxf(m0, m);
-        s = st.s[row] * expf(m0 - m1) + s * expf(m - m1);
-        m = m1;
-      } else {
-        st.zy[row] = NAN;  // no label met yet
-      }
-      st.m[row] = m;
-      st.s[row] = s;
-      const int64_t at = (int64_t)y[row] - c0;
-      if (at >= 0 && at < width) st.zy[row] = r[at];
+  const int64_t i = (int64_t)blockIdx.x * kRowsPerBlock + threadIdx.x;
+  const int c = __syncthreads_count(i < n && mask[i] != 0);
+  if (threadIdx.x == 0) counts[blockIdx.x] = c;
+}
+// place[i] = how many counted rows lie before row i, -1 where i does not count or is beyond the `room` places; rows[place] = i
+// (-1 behind the last one), *total = all that count.
+__global__ void __launch_bounds__(kRowsPerBlock)
+mask_places(int64_t n, const uint8_t* __restrict__ mask, const int* __restrict__ counts, int64_t room, int32_t* __restrict__ place,
+            int32_t* __restrict__ rows, int* __restrict__ total) {
+  wait_for_predecessors();
+  __shared__ int sh[32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  int before = 0;  // rows that count in the blocks before
+  for (int b = threadIdx.x; b < (int)blockIdx.x; b += kRowsPerBlock) before += counts[b];
+  before = __reduce_add_sync(kFull, before);
+  if (lane == 0) sh[w] = before;
+  __syncthreads();
+  before = __reduce_add_sync(kFull, sh[lane]);
+  __syncthreads();
+  const int64_t i = (int64_t)blockIdx.x * kRowsPerBlock + threadIdx.x;
+  const bool on = i < n && mask[i] != 0;
+  const unsigned set = __ballot_sync(kFull, on);
+  if (lane == 0) sh[w] = __popc(set);
+  __syncthreads();
+  const int mine = sh[lane];
+  int warps = __reduce_add_sync(kFull, lane < w ? mine : 0), all = __reduce_add_sync(kFull, mine);
+  const int64_t at = (int64_t)before + warps + __popc(set & ((1u << lane) - 1));
+  if (i < n) place[i] = on && at < room ? (int32_t)at : -1;
+  if (on && at < room) rows[at] = (int32_t)i;
+  if (blockIdx.x == gridDim.x - 1) {
+    const int64_t count = (int64_t)before + all;
+    if (threadIdx.x == 0) *total = (int)count;
+    for (int64_t k = count + threadIdx.x; k < room; k += kRowsPerBlock) rows[k] = -1;
+  }
+}
+// A warp per row: counted rows of h and their labels to their places, rows of dh that do not count to zero.  Places behind
+// the last counted row (n_train larger than the mask says) become rows of zeros without a label.
+__global__ void __launch_bounds__(256)
+gather_rows(int64_t n, int d, const float* __restrict__ h, int64_t ldh, const int32_t* __restrict__ y, const int32_t* __restrict__ place,
+            const int* __restrict__ total, int64_t room, float* __restrict__ hc, int64_t ldc, int32_t* __restrict__ yc, float* __restrict__ dh, int64_t lddh) {
+  wait_for_predecessors();
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const bool vec = ((uintptr_t)h & 15) == 0 && ldh % 4 == 0;
+  const int pad = (int)min(lddh, (int64_t)(d + 3) / 4 * 4);
+  for (int64_t i = (int64_t)blockIdx.x * 8 + w; i < n; i += (int64_t)gridDim.x * 8) {
+    const int at = place[i];
+    if (at >= 0) {
+      const float* src = h + i * ldh;
+      float* dst = hc + at * ldc;
+      const int d4 = vec ? d / 4 : 0;
+      for (int j = lane; j < d4; j += 32) reinterpret_cast<float4*>(dst)[j] = __ldg(reinterpret_cast<const float4*>(src) + j);
+      for (int j = 4 * d4 + lane; j < d; j += 32) dst[j] = __ldg(src + j);
+      if (lane == 0) yc[at] = y[i];
+    } else if (dh) {
+      for (int j = lane; j < pad; j += 32) dh[i * lddh + j] = 0.f;
     }
   }
-}
-__global__ void __launch_bounds__(256)
-ce_piece_grad(int64_t n, int c0, int width, int pad, float* __restrict__ z, int64_t ldz, const int32_t* __restrict__ y,
-              const uint8_t* __restrict__ mask, float inv_nt, RowState st) {
-  wait_for_predecessors();
-  const int lane = threadIdx.x & 31;
-  for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += (int64_t)gridDim.x * 8) {
-    float* r = z + row * ldz;
-    const bool on = !mask || mask[row] != 0;
-    const float m = st.m[row], inv = 1.f / st.s[row];
-    const int yi = y[row];
-    for (int j = lane; j < pad; j += 32)
-      r[j] = on && j < width ? (expf(r[j] - m) * inv - (c0 + j == yi ? 1.f : 0.f)) * inv_nt : 0.f;
+  for (int64_t k = (int64_t)*total + (int64_t)blockIdx.x * 8 + w; k < room; k += (int64_t)gridDim.x * 8) {
+    for (int j = lane; j < d; j += 32) hc[k * ldc + j] = 0.f;
+    if (lane == 0) yc[k] = -1;
   }
 }
-// sum of the masked rows' losses and their number, in a fixed order
-__global__ void __launch_bounds__(1024)
-ce_loss(int64_t n, const uint8_t* __restrict__ mask, RowState st, int64_t n_train, float* __restrict__ loss) {
+
+// logsumexp of every row from the runs that crossed its tile, and its loss
+__global__ void __launch_bounds__(256)
+row_finish(int64_t rows, int tiles_n, int total, int grid, const float* __restrict__ part_m, const float* __restrict__ part_s,
+           const float* __restrict__ zy, float* __restrict__ lse, float* __restrict__ row_loss) {
   wait_for_predecessors();
-  __shared__ double sh[32];
-  __shared__ long long shc[32];
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows) return;
+  const int t = (int)(r / BM);
+  const int b0 = term_owner(t * tiles_n, total, grid), b1 = term_owner((t + 1) * tiles_n - 1, total, grid);
+  float m = -INFINITY, s = 0.f;
+  for (int b = b0; b <= b1; ++b)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t slot = ((int64_t)(b + t) * 2 + h) * BM + r % BM;
+      const float pm = part_m[slot], top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
+      s = s * expf(m - base) + part_s[slot] * expf(pm - base);
+      m = top;
+    }
+  const float l = (m == -INFINITY ? 0.f : m) + logf(s);
+  lse[r] = l;
+  row_loss[r] = l - zy[r];
+}
+// Sums of row losses and the number of rows that count, a partial of both per block; the block that is alone finishes.
+struct LossSum {
+  double loss;
+  long long count;
+};
+__device__ __forceinline__ void finish_loss(const LossSum& s, long long count, int64_t n_train, float* loss) {
+  *loss = count != n_train ? NAN : n_train > 0 ? (float)(s.loss / (double)n_train) : 0.f;
+}
+constexpr int kLossThreads = 512, kLossBlocks = 148;
+// mask (with rows that are not gathered): counted here; total: counted before; neither: all rows count
+__global__ void __launch_bounds__(kLossThreads)
+loss_sums(int64_t rows, const float* __restrict__ row_loss, const uint8_t* __restrict__ mask, const int* __restrict__ total,
+          int64_t n_train, LossSum* __restrict__ partial, float* __restrict__ loss) {
+  wait_for_predecessors();
+  __shared__ double shl[kLossThreads / 32];
+  __shared__ int shc[kLossThreads / 32];
   double s = 0.0;
-  long long count = 0;
-  for (int64_t row = threadIdx.x; row < n; row += 1024)
-    if (!mask || mask[row]) {
-      s += (double)(st.m[row] + logf(st.s[row])) - st.zy[row];
-      ++count;
-    }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    s += __shfl_xor_sync(kFull, s, o);
-    count += __shfl_xor_sync(kFull, count, o);
+  int count = 0;
+#pragma unroll 4
+  for (int64_t r = (int64_t)blockIdx.x * kLossThreads + threadIdx.x; r < rows; r += (int64_t)gridDim.x * kLossThreads) {
+    s += row_loss[r];
+    count += !mask || mask[r] != 0;
   }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  count = __reduce_add_sync(kFull, count);
   if ((threadIdx.x & 31) == 0) {
-    sh[threadIdx.x >> 5] = s;
+    shl[threadIdx.x >> 5] = s;
     shc[threadIdx.x >> 5] = count;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 32; ++w) {
-      s += sh[w];
-      count += shc[w];
-    }
-    *loss = count != n_train ? NAN : n_train > 0 ? (float)(s / (double)n_train) : 0.f;
+  if (threadIdx.x != 0) return;
+  LossSum a = {0.0, 0};
+  for (int w = 0; w < kLossThreads / 32; ++w) {
+    a.loss += shl[w];
+    a.count += shc[w];
   }
+  if (gridDim.x == 1) finish_loss(a, total ? *total : a.count, n_train, loss);
+  else partial[blockIdx.x] = a;
+}
+__global__ void __launch_bounds__(32)
+loss_total(int blocks, const LossSum* __restrict__ partial, const int* __restrict__ total, int64_t n_train, float* __restrict__ loss) {
+  wait_for_predecessors();
+  if (threadIdx.x != 0) return;
+  LossSum a = {0.0, 0};
+  for (int b = 0; b < blocks; ++b) {
+    a.loss += partial[b].loss;
+    a.count += partial[b].count;
+  }
+  finish_loss(a, total ? *total : a.count, n_train, loss);
+}
+// out[j] (+)= sum over `lines` lines of sums[i * pitch + j]
+__global__ void __launch_bounds__(256)
+sum_lines(int n, int lines, const float* __restrict__ sums, int64_t pitch, float* __restrict__ out, int accumulate) {
+  wait_for_predecessors();
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= n) return;
+  float s = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < lines; ++i) s += sums[i * pitch + j];
+  out[j] = accumulate ? out[j] + s : s;
 }
 
-int64_t piece_of(int64_t n, int32_t c) {
-  const int64_t fit = (int64_t(64) << 20) / 4 / std::max<int64_t>(n, 1) / 128 * 128;
-  return std::min<int64_t>((c + 3) / 4 * 4, std::max<int64_t>(fit, 128));
+// ---- plan of a call: sizes that hold for every count of rows up to n -------------------------------------------------
+constexpr int kWholeCols = 128;                    // classes that one tile holds
+constexpr int64_t kPieceFloats = int64_t(16) << 20;  // of G^T: half of L2
+struct CePlan {
+  int64_t gt_floats, partial_floats, sums_floats, slots;
+  size_t gt, partial, sums, hc, wc, yc, rows, place, counts, total, zy, lse, row_loss, part, losses, end;
+};
+CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
+  CePlan p;
+  const int64_t n4 = up4(n), c128 = div_up(c, 128) * 128, sms = sm_count();
+  const bool whole = c <= kWholeCols;
+  p.gt_floats = whole ? c * n4 : std::min(c128 * n4, std::max(kPieceFloats, 128 * n4));
+  // at most 2 x SMs items of slices of dW^T (pick_slices)
+  p.partial_floats = n > 0 ? std::min(2 * sms, std::max<int64_t>(div_up(n, BK), 1) * div_up(d, 128) * (c128 / 128)) * 128 * 128 : 0;
+  p.sums_floats = n > 0 ? 2 * std::max<int64_t>(2 * sms * 128, c128) : 0;  // two lines per slice
+  p.slots = sms + div_up(n, BM);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += up256(bytes); return o; };
+  p.gt = take((size_t)p.gt_floats * 4);
+  p.partial = take((size_t)p.partial_floats * 4);
+  p.sums = take((size_t)p.sums_floats * 4);
+  p.hc = take((size_t)n * up4(d) * 4);
+  p.wc = take((size_t)d * up4(c) * 4);
+  p.yc = take((size_t)n * 4);
+  p.rows = take((size_t)n * 4);
+  p.place = take((size_t)n * 4);
+  p.counts = take((size_t)div_up(n, kRowsPerBlock) * 4);
+  p.total = take(4);
+  p.zy = take((size_t)n * 4);
+  p.lse = take((size_t)n * 4);
+  p.row_loss = take((size_t)n * 4);
+  p.part = take((size_t)p.slots * 2 * BM * 2 * 4);
+  p.losses = take(kLossBlocks * sizeof(LossSum));
+  p.end = at;
+  return p;
 }
+// Classes of a piece: a multiple of 128 whose G^T fits its room, and from the upper half of those the one whose tiles fill
+// the rounds over the SMs best.
+int64_t piece_classes(const CePlan& p, int64_t rows, int32_t c) {
+  const int64_t all = div_up(c, 128), most = std::max<int64_t>(1, std::min(all, p.gt_floats / (128 * up4(rows)))), tiles_m = div_up(rows, BM), sms = sm_count();
+  int64_t best = most;
+  double best_cost = 1e30;
+  for (int64_t k = most; k >= std::max<int64_t>(1, most / 2); --k) {
+    const double cost = (double)div_up(tiles_m * k, sms) / (double)k;
+    if (cost < best_cost - 1e-9) {
+      best = k;
+      best_cost = cost;
+    }
+  }
+  return best * 128;
+}
+
+#define GCNSA_STEP(...)                           \
+  do {                                            \
+    const int rc_ = (int)(__VA_ARGS__);           \
+    if (rc_ != 0) return rc_;                     \
+  } while (0)
 
 }  // namespace
 
 size_t gemm_packed8_workspace(int64_t n, int32_t f, int32_t c) {
-  return up256((size_t)packed8_slices(n, f, c) * f * (((size_t)c + 3) / 4 * 4) * sizeof(float));
+  const PackedPlan p = packed_plan(n, f, c);
+  return p.slices > 1 ? up256((size_t)p.slices * f * p.ldp * sizeof(float)) : 0;
 }
 
 int launch_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g, int64_t ldg,
                         float* dw, int64_t lddw, int32_t accumulate, void* workspace) {
-  const int64_t ldp = ((int64_t)c + 3) / 4 * 4;
-  const int slices = n > 0 ? packed8_slices(n, f, c) : 0;
-  if (n > 0) {
-    const dim3 grid((f + kTile - 1) / kTile, (c + kTile - 1) / kTile, slices);
-    launch(packed8_product, grid, 256, 0, (cudaStream_t)stream, n, f, c, *x, g, ldg, (n + slices - 1) / slices, (float*)workspace, ldp);
-    note_launch();
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return (int)e;
-  }
-  return launch_splitk_reduce(stream, f, c, slices, (const float*)workspace, ldp, dw, lddw, accumulate, GCNSA_EPI_NONE, nullptr, 0);
+  if (n <= 0) return launch_splitk_reduce(stream, f, c, 0, nullptr, up4(c), dw, lddw, accumulate, GCNSA_EPI_NONE, nullptr, 0);
+  const PackedPlan pl = packed_plan(n, f, c);
+  const bool tma = ((uintptr_t)g & 15) == 0 && ldg % 4 == 0;
+  TermArgs a = {};
+  Product& p = a.p[0];
+  if (!term_map(&p.map_b, x->q, true, n, f, x->ldq, pl.bn, BK, false) || (tma && !term_map(&p.map_a, g, false, n, c, ldg, 32, BK, false)))
+    return (int)cudaErrorNotSupported;
+  p.M = c;
+  p.N = f;
+  p.units = (int)div_up(n, BK);
+  set_slices(p, pl.bn, pl.slices);
+  const bool split = pl.slices > 1;
+  p.c = split ? (float*)workspace : dw;
+  p.ldc = split ? pl.ldp : lddw;
+  p.slice_stride = split ? f * pl.ldp : 0;
+  p.accumulate = split ? 0 : accumulate;
+  p.m_pad = (int)std::min<int64_t>(p.ldc, up4(c));
+  p.write = 1;
+  p.a = g;
+  p.lda = ldg;
+  p.k_rows = n;
+  p.e = x->e;
+  p.lde = x->lde;
+  p.e_blocks = (int)div_up(f, kPackBlock);
+  a.total = p.items;
+  const int grid = std::min(a.total, sm_count());
+  cudaStream_t s = (cudaStream_t)stream;
+  GCNSA_STEP(pl.bn == 64 ? (tma ? run_packed<64, ASrc::mnMajor>(s, a, grid) : run_packed<64, ASrc::direct>(s, a, grid))
+                         : (tma ? run_packed<128, ASrc::mnMajor>(s, a, grid) : run_packed<128, ASrc::direct>(s, a, grid)));
+  note_launch();
+  if (split) return launch_splitk_reduce(stream, f, c, pl.slices, (const float*)workspace, pl.ldp, dw, lddw, accumulate, GCNSA_EPI_NONE, nullptr, 0);
+  return 0;
 }
 
-size_t linear_ce_workspace(int64_t n, int32_t d, int32_t c) {
-  const int64_t piece = piece_of(n, c);
-  return up256((size_t)n * piece * 4) + 3 * up256((size_t)n * 4) + up256(colsum_scratch(n, (int32_t)piece)) +
-         up256(std::max({gemm_workspace(GCNSA_GEMM_FP32, 0, 0, n, piece, d), gemm_workspace(GCNSA_GEMM_FP32, 0, 1, n, d, piece),
-                         gemm_workspace(GCNSA_GEMM_FP32, 1, 0, d, piece, n)}));
-}
+size_t linear_ce_workspace(int64_t n, int32_t d, int32_t c) { return ce_plan(n, d, c).end; }
 
 int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
   cudaStream_t s = (cudaStream_t)stream;
-  const int64_t n = a.n, piece = piece_of(n, a.c);
-  uint8_t* ws = (uint8_t*)workspace;
-  auto take = [&](size_t bytes) { uint8_t* p = ws; ws += up256(bytes); return p; };
-  float* z = (float*)take((size_t)n * piece * 4);
-  RowState st;
-  st.m = (float*)take((size_t)n * 4);
-  st.s = (float*)take((size_t)n * 4);
-  st.zy = (float*)take((size_t)n * 4);
-  void* sums = take(colsum_scratch(n, (int32_t)piece));
-  void* gw = ws;
-  const size_t gwb = (size_t)((uint8_t*)workspace + linear_ce_workspace(n, a.d, a.c) - ws);
+  const CePlan pl = ce_plan(a.n, a.d, a.c);
+  uint8_t* const ws = (uint8_t*)workspace;
+  auto f_at = [&](size_t o) { return (float*)(ws + o); };
+  const int sms = sm_count();
+  const bool whole = a.c <= kWholeCols, grads = a.dh || a.dw || a.db;
   const float inv_nt = a.n_train > 0 ? 1.f / (float)a.n_train : 0.f;
-  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>((n + 7) / 8, 148 * 8));
-#define GCNSA_STEP(call)              \
-  do {                                \
-    const int rc_ = (call);           \
-    if (rc_ != 0) return rc_;         \
-  } while (0)
-  auto logits = [&](int64_t c0, int64_t width) {
-    return launch_gemm(stream, GCNSA_GEMM_FP32, 0, 0, n, width, a.d, a.h, a.ldh, a.w + c0, a.ldw, z, piece, 0, a.bias ? GCNSA_EPI_BIAS : GCNSA_EPI_NONE,
-                       a.bias ? a.bias + c0 : nullptr, 0, gw, gwb);
-  };
-  if (n > 0)
-    for (int64_t c0 = 0; c0 < a.c; c0 += piece) {
-      const int64_t width = std::min<int64_t>(piece, a.c - c0);
-      GCNSA_STEP(logits(c0, width));
-      launch(ce_piece_stats, blocks, 256, 0, s, n, (int)c0, (int)width, (const float*)z, piece, a.y, st);
+  const int *total = nullptr;
+  const int32_t *rows = nullptr, *y = a.y;
+  const float *h = a.h, *w = a.w;
+  int64_t ldh = a.ldh, ldw = a.ldw, R = a.n;  // rows of the products
+
+  const bool gather = !whole && a.mask && a.n > 0;
+  if (gather) {
+    const int blocks = (int)div_up(a.n, kRowsPerBlock);
+    R = a.n_train;
+    GCNSA_STEP(launch(mask_counts, blocks, kRowsPerBlock, 0, s, a.n, a.mask, (int*)(ws + pl.counts)));
+    GCNSA_STEP(launch(mask_places, blocks, kRowsPerBlock, 0, s, a.n, a.mask, (const int*)(ws + pl.counts), R, (int32_t*)(ws + pl.place),
+                      (int32_t*)(ws + pl.rows), (int*)(ws + pl.total)));
+    GCNSA_STEP(launch(gather_rows, (int)std::min<int64_t>(div_up(a.n, 8), 148 * 8), 256, 0, s, a.n, a.d, a.h, a.ldh, a.y,
+                      (const int32_t*)(ws + pl.place), (const int*)(ws + pl.total), R, f_at(pl.hc), up4(a.d), (int32_t*)(ws + pl.yc), a.dh, a.lddh));
+    note_launch(3);
+    h = f_at(pl.hc);
+    ldh = up4(a.d);
+    y = (const int32_t*)(ws + pl.yc);
+    rows = (const int32_t*)(ws + pl.rows);
+    total = (const int*)(ws + pl.total);
+  } else if (a.n > 0 && (((uintptr_t)h & 15) || ldh % 4)) {  // TMA wants lines on 16-byte boundaries
+    GCNSA_STEP(launch_copy_rows(stream, a.n, a.d, a.h, a.ldh, f_at(pl.hc), up4(a.d)));
+    h = f_at(pl.hc);
+    ldh = up4(a.d);
+  }
+  if (R > 0 && (((uintptr_t)w & 15) || ldw % 4)) {
+    GCNSA_STEP(launch_copy_rows(stream, a.d, a.c, a.w, a.ldw, f_at(pl.wc), up4(a.c)));
+    w = f_at(pl.wc);
+    ldw = up4(a.c);
+  }
+
+  const int64_t ldg = up4(R);
+  TermArgs t = {};  // z
+  t.ce.bias = a.bias;
+  t.ce.y = y;
+  t.ce.ldg = (int)ldg;
+  t.ce.inv_nt = inv_nt;
+  if (R > 0) {
+    Product& p = t.p[0];
+    if (!term_map(&p.map_a, h, false, R, a.d, ldh, BK, BM, true) || !term_map(&p.map_b, w, false, a.d, a.c, ldw, 32, BK, false))
+      return (int)cudaErrorNotSupported;
+    p.M = (int)R;
+    p.N = a.c;
+    p.units = (int)div_up(a.d, BK);
+    p.k_rows = a.d;
+  }
+  // loss
+  if (R > 0 && whole) {
+    t.ce.mask = a.mask;
+    t.ce.gt = grads ? f_at(pl.gt) : nullptr;
+    t.ce.row_loss = f_at(pl.row_loss);
+    set_slices(t.p[0], a.c <= 64 ? 64 : 128, 1);
+    t.total = t.p[0].items;
+    const int grid = std::min(t.total, sms);
+    GCNSA_STEP(a.c <= 64 ? run_terms<TermShape<64, ASrc::kMajor, false, Out::whole>>(s, t, grid)
+                         : run_terms<TermShape<128, ASrc::kMajor, false, Out::whole>>(s, t, grid));
+    note_launch();
+  } else if (R > 0) {
+    GCNSA_STEP(cudaMemsetAsync(ws + pl.zy, 0xff, (size_t)R * 4, s));  // NaN: no class was the row's label
+    t.ce.zy = f_at(pl.zy);
+    t.ce.part_m = f_at(pl.part);
+    t.ce.part_s = f_at(pl.part) + pl.slots * 2 * BM;
+    set_slices(t.p[0], 128, 1);
+    t.total = t.p[0].items;
+    const int grid = std::min(t.total, sms);
+    GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::stats>>(s, t, grid)));
+    GCNSA_STEP(launch(row_finish, (int)div_up(R, 256), 256, 0, s, R, t.p[0].tiles_n, t.total, grid, (const float*)t.ce.part_m, (const float*)t.ce.part_s,
+                      (const float*)t.ce.zy, f_at(pl.lse), f_at(pl.row_loss)));
+    note_launch(2);
+    t.ce.lse = f_at(pl.lse);
+  }
+  {
+    const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(div_up(R, 16 * kLossThreads), kLossBlocks));
+    GCNSA_STEP(launch(loss_sums, blocks, kLossThreads, 0, s, R, (const float*)f_at(pl.row_loss), whole ? a.mask : nullptr, total, a.n_train,
+                      (LossSum*)(ws + pl.losses), a.loss));
+    if (blocks > 1) GCNSA_STEP(launch(loss_total, 1, 32, 0, s, blocks, (const LossSum*)(ws + pl.losses), total, a.n_train, a.loss));
+    note_launch(blocks > 1 ? 2 : 1);
+  }
+  if (!grads) return 0;
+  if (R == 0) {  // nothing counts: sums of nothing
+    if (a.dw) GCNSA_STEP(launch_splitk_reduce(stream, a.d, a.c, 0, nullptr, up4(a.c), a.dw, a.lddw, a.accumulate, GCNSA_EPI_NONE, nullptr, 0));
+    if (a.db) {
+      GCNSA_STEP(launch(sum_lines, (int)div_up(a.c, 256), 256, 0, s, a.c, 0, (const float*)nullptr, (int64_t)0, a.db, a.accumulate));
       note_launch();
     }
-  launch(ce_loss, 1, 1024, 0, s, n, a.mask, st, a.n_train, a.loss);
-  note_launch();
-  GCNSA_STEP((int)cudaGetLastError());
-  if (!a.dh && !a.dw && !a.db) return 0;
+    return 0;
+  }
+  const int64_t piece = whole ? a.c : piece_classes(pl, R, a.c);
   for (int64_t c0 = 0; c0 < a.c; c0 += piece) {
     const int64_t width = std::min<int64_t>(piece, a.c - c0);
-    if (n > 0) {
-      if (piece < a.c) GCNSA_STEP(logits(c0, width));
-      launch(ce_piece_grad, blocks, 256, 0, s, n, (int)c0, (int)width, (int)((width + 3) / 4 * 4), z, piece, a.y, a.mask, inv_nt, st);
+    if (!whole) {
+      if (!term_map(&t.p[0].map_b, w + c0, false, a.d, width, ldw, 32, BK, false)) return (int)cudaErrorNotSupported;
+      t.p[0].N = (int)width;
+      t.ce.c0 = (int)c0;
+      t.ce.gt = f_at(pl.gt);
+      set_slices(t.p[0], 128, 1);
+      t.total = t.p[0].items;
+      GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::grad>>(s, t, std::min(t.total, sms))));
       note_launch();
-      if (a.dh) GCNSA_STEP(launch_gemm(stream, GCNSA_GEMM_FP32, 0, 1, n, a.d, width, z, piece, a.w + c0, a.ldw, a.dh, a.lddh, c0 > 0, GCNSA_EPI_NONE, nullptr, 0, gw, gwb));
     }
-    if (a.dw) GCNSA_STEP(launch_gemm(stream, GCNSA_GEMM_FP32, 1, 0, a.d, width, n, a.h, a.ldh, z, piece, a.dw + c0, a.lddw, a.accumulate, GCNSA_EPI_NONE, nullptr, 0, gw, gwb));
-    if (a.db) GCNSA_STEP(launch_colsum(stream, n, (int32_t)width, z, piece, a.db + c0, a.accumulate, sums));
+    TermArgs b = {};
+    Product &pw = b.p[0], &ph = b.p[1];
+    const bool weights = a.dw || a.db;
+    int slices = 1;
+    if (weights) {
+      if (!term_map(&pw.map_a, f_at(pl.gt), false, width, R, ldg, BK, BM, true) || !term_map(&pw.map_b, h, false, R, a.d, ldh, 32, BK, false))
+        return (int)cudaErrorNotSupported;
+      pw.M = (int)width;
+      pw.N = a.d;
+      pw.units = (int)div_up(R, BK);
+      slices = pick_slices(div_up(width, BM) * div_up(a.d, 128), pw.units);
+      set_slices(pw, 128, slices);
+      const bool split = slices > 1;
+      pw.write = a.dw != nullptr;
+      pw.c = split ? f_at(pl.partial) : a.dw + (a.dw ? c0 : 0);
+      pw.ldc = split ? up4(width) : a.lddw;
+      pw.slice_stride = split ? a.d * up4(width) : 0;
+      pw.accumulate = split ? 0 : a.accumulate;
+      // pad columns belong to the last piece
+      pw.m_pad = (int)(split ? up4(width) : c0 + width < a.c ? width : std::min<int64_t>(a.lddw - c0, up4(width)));
+      pw.k_rows = R;
+      if (a.db) {
+        pw.a_sums = f_at(pl.sums);
+        pw.sums_pitch = up4(width);
+      }
+    }
+    if (a.dh) {
+      if (!term_map(&ph.map_a, w + c0, false, a.d, width, ldw, BK, BM, true) || !term_map(&ph.map_b, f_at(pl.gt), false, width, R, ldg, 32, BK, false))
+        return (int)cudaErrorNotSupported;
+      ph.M = a.d;
+      ph.N = (int)R;
+      ph.units = (int)div_up(width, BK);
+      set_slices(ph, 128, 1);
+      ph.write = 1;
+      ph.c = a.dh;
+      ph.ldc = a.lddh;
+      ph.row_map = rows;
+      ph.accumulate = c0 > 0;
+      ph.m_pad = (int)std::min<int64_t>(a.lddh, up4(a.d));
+      ph.k_rows = width;
+    }
+    b.total = pw.items + ph.items;
+    GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::transposed>>(s, b, std::min(b.total, sms))));
+    note_launch();
+    if (a.dw && slices > 1)
+      GCNSA_STEP(launch_splitk_reduce(stream, a.d, width, slices, (const float*)f_at(pl.partial), up4(width), a.dw + c0, a.lddw, a.accumulate, GCNSA_EPI_NONE, nullptr, 0));
+    if (a.db) {
+      GCNSA_STEP(launch(sum_lines, (int)div_up(width, 256), 256, 0, s, (int)width, 2 * slices, (const float*)f_at(pl.sums), up4(width), a.db + c0, a.accumulate));
+      note_launch();
+    }
   }
-#undef GCNSA_STEP
   return 0;
+}
+
+int tc_status_head(int* out) {
+  int v = 0;
+  cudaError_t e = cudaMemcpyFromSymbol(&v, g_tc_error, sizeof(int));
+  if (e != cudaSuccess) return (int)e;
+  *out = v;
+  return 0;
+}
+
+int tc_clear_head() {
+  const int zero = 0;
+  return (int)cudaMemcpyToSymbol(g_tc_error, &zero, sizeof(int));
 }
 
 }  // namespace gcnsa

@@ -605,17 +605,21 @@ int debug_word_dense(unsigned long long* out, bool clear) {
 }
 
 int tc_status(int* out) {
-  int v = 0, w = 0;
+  int v = 0, w = 0, h = 0;
   cudaError_t e = cudaMemcpyFromSymbol(&v, g_tc_error, sizeof(int));
   if (e != cudaSuccess) return (int)e;
   const int r = tc_status_gemm(&w);
-  *out = w ? w : v;
-  return r;
+  if (r) return r;
+  const int r2 = tc_status_head(&h);
+  *out = w ? w : v ? v : h;
+  return r2;
 }
 int tc_clear() {
   const int zero = 0;
   cudaError_t e = cudaMemcpyToSymbol(g_tc_error, &zero, sizeof(int));
-  return e != cudaSuccess ? (int)e : tc_clear_gemm();
+  if (e != cudaSuccess) return (int)e;
+  const int r = tc_clear_gemm();
+  return r ? r : tc_clear_head();
 }
 
 }  // namespace gcnsa

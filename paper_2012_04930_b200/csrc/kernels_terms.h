@@ -1,0 +1,668 @@
+// D = A B on the 5th-generation tensor cores from bf16 terms, with sums that keep fp32 accuracy however long they are.
+//
+// A fp32 value is the exact sum of three bf16 terms (24 significant bits cut into 8 + 8 + 8); of the nine products of two
+// such operands the three smallest lie below 2^-22 of the product and are left out.  An operand that is an 8-bit checkpoint
+// is one bf16 term.  The tensor core cuts a sum off at 24 bits, always toward zero, where an fp32 addition rounds, so an
+// accumulator may not live long: the products of the leading terms go into one of two accumulators in turn, two
+// instructions per 32 k, and after kFoldUnits x 32 k its sum is added to running sums in registers (rounded), while the
+// MMAs go on in the other one.  The products of the smaller terms have a third accumulator; what is cut off there is
+// 2^-8 of that, and it is folded every kSmallFolds folds.  (One accumulator for everything over 245 000 rows would be
+// 1e-4 off.)
+//
+// One CTA per SM works on tiles of 128 x BN.  Warps 0 and 2 stream boxes of A and B into rings of shared memory with TMA;
+// two groups of four warps (4-11) take every other k-block each: A goes as three terms into tensor memory (a lane per row
+// of the tile, two k per 32-bit column), B as one or three terms into MN-major tiles with the 128-byte swizzle.  Warp 1
+// issues the MMAs, and eight warps (12-19, two per lane quarter of tensor memory, half the columns each) fold the
+// accumulators and write the result: thread = row of the tile, so a result that is wanted transposed, D[m, n] at
+// c[n * ldc + m], is written in lines of 128 bytes without a turn through shared memory.  Every product of this file is
+// arranged so that this is the layout it needs.
+//
+// A k-block of 32 of a 128 x 128 tile keeps the tensor pipe busy for 768 clocks (12 MMAs) and shared memory for about
+// 1 090 (boxes in 256, both read for the split 256, terms of B out 192, B read by the MMAs 384, at 128 bytes a clock): the
+// latter is what bounds the fp32 x fp32 products.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "launch.h"
+#include "pack8_device.h"
+#include "tc_device.h"
+#include "tma_host.h"
+
+namespace gcnsa {
+namespace {
+
+constexpr int BM = 128, BK = 32;
+constexpr int kConvWarp0 = 4, kConvGroups = 2, kFoldWarp0 = 12, kFoldWarps = 8, kTermThreads = 32 * (kFoldWarp0 + kFoldWarps);
+// registers per thread by role, in multiples of 8; their sum over the five warpgroups is what the launch gives (96 each)
+constexpr int kRegsIssue = 48, kRegsConv = 80, kRegsFold = 136;
+static_assert(kRegsIssue + 2 * kRegsConv + 2 * kRegsFold <= 5 * 96, "setmaxnreg draws on the registers of the launch");
+constexpr int kFoldUnits = 8, kSmallFolds = 8;
+constexpr int A_SLOT = BM * BK * 4;
+
+// A: K-major (k contiguous in memory), MN-major (rows of D contiguous), or MN-major without the alignment that TMA needs
+// (read with plain loads)
+enum class ASrc { kMajor, mnMajor, direct };
+enum class Out { transposed, stats, grad, whole };
+
+// D[m, n] = sum_k A[m, k] B[k, n], B MN-major
+struct Product {
+  CUtensorMap map_a, map_b;
+  int M, N, units, per_slice, tiles_m, tiles_n, items;  // units: k-blocks of 32; items = tiles x slices
+  float* c;                // element (m, n) at c[z * slice_stride + row(n) * ldc + m]
+  int64_t ldc, slice_stride;
+  const int32_t* row_map;  // row(n), nullable; negative: not written
+  int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros
+  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of parity g: a_sums[(2 z + g) * sums_pitch + m]
+  int64_t sums_pitch;
+  int write;               // 0: only a_sums are wanted
+  const float* a;          // ASrc::direct
+  int64_t lda, k_rows;
+  const uint8_t* e;        // steps of a packed B
+  int64_t lde;
+  int e_blocks;
+};
+// The epilogues of the output layer; D[m, n] is a logit without its bias, m a row, n a class of the piece from c0 on.
+struct CeTile {
+  const float* bias;     // nullable, of the whole layer
+  const int32_t* y;      // [M]
+  const uint8_t* mask;   // nullable [M] (Out::whole)
+  int c0, ldg;
+  float inv_nt;
+  float* gt;             // G^T: [class of the piece][ldg]; nullable (Out::whole)
+  const float* lse;      // [M] (Out::grad)
+  float *part_m, *part_s, *zy;  // (Out::stats) running maximum and sum of a CTA's run in a row tile, the label's logit
+  float* row_loss;       // [M] (Out::whole)
+};
+struct TermArgs {
+  Product p[2];
+  CeTile ce;
+  int total;  // items of both
+};
+
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
+      : "memory");
+}
+// MN-major tile of 16-bit elements, 128-byte swizzle: blocks of 64 n x 32 k (4 096 bytes apart), in a block the 64 elements of
+// one k are 128 contiguous bytes and 8 k are a swizzle group of 1 024 bytes.
+__device__ __forceinline__ uint64_t desc_b(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFF) >> 4);
+  d |= (uint64_t)(4096 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n"
+      " .reg .pred p;\n"
+      " setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+// Two values as three pairs of bf16 terms, the first value in the lower halves.  The leading term is cut off, so that no
+// finite value becomes an infinity; what is left of it is exact, the second term is rounded, and the third holds the rest
+// exactly.
+__device__ __forceinline__ void split3(float x0, float x1, uint32_t& t0, uint32_t& t1, uint32_t& t2) {
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(t0) : "f"(x1), "f"(x0));
+  x0 -= __uint_as_float(t0 << 16);
+  x1 -= __uint_as_float(t0 & 0xffff0000u);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(t1) : "f"(x1), "f"(x0));
+  x0 -= __uint_as_float(t1 << 16);
+  x1 -= __uint_as_float(t1 & 0xffff0000u);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(t2) : "f"(x1), "f"(x0));
+}
+
+template <int BN_, ASrc A_, bool P8_, Out OUT_>
+struct TermShape {
+  static constexpr int BN = BN_;
+  static constexpr ASrc A = A_;
+  static constexpr bool P8 = P8_;
+  static constexpr Out OUT = OUT_;
+  static constexpr int NTB = P8 ? 1 : 3;                 // terms of B
+  static constexpr int HALF = BN / 2;                    // columns of a fold warp
+  static constexpr int A_COLS = 48;                      // tensor-memory columns of a stage of A
+  static constexpr int NSA = BN == 64 ? 4 : 2, NSB = 3;  // stages of terms
+  static constexpr int A_COL0 = 3 * BN, TMEM_COLS = 512;
+  static constexpr int B_SLOT = BK * BN * (P8 ? 1 : 4), B_TERM = BK * BN * 2;
+  static constexpr int NA = A == ASrc::direct ? 0 : 4, NB = P8 ? 8 : 4;  // landing slots
+  static constexpr int B_OFF = NA * A_SLOT, T_OFF = B_OFF + NB * B_SLOT, X_OFF = T_OFF + NSB * NTB * B_TERM;
+  static constexpr int X_BYTES = OUT == Out::whole ? 2 * 2 * BM * 4 : 0;  // maxima and sums of the halves of a row
+  static constexpr int BAR_OFF = X_OFF + X_BYTES;
+  // more than half of an SM's shared memory: a second CTA, which would wait for tensor memory, never shares the SM
+  static constexpr int NEED = BAR_OFF + 512 + 1024;
+  static constexpr int SMEM_BYTES = NEED > 118 * 1024 ? NEED : 118 * 1024;
+  static_assert(A_COL0 + NSA * A_COLS <= TMEM_COLS, "tensor memory has 512 columns");
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
+};
+
+struct TermWork {
+  int prob, m0, n0, z, kb0, n_kb;
+};
+__device__ __forceinline__ TermWork term_work(const TermArgs& a, int w, int bn) {
+  TermWork k;
+  k.prob = w >= a.p[0].items;
+  if (k.prob) w -= a.p[0].items;
+  const Product& p = a.p[k.prob];
+  const int tiles = p.tiles_m * p.tiles_n;
+  k.z = w / tiles;
+  w -= k.z * tiles;
+  k.m0 = w / p.tiles_n * BM;
+  k.n0 = w % p.tiles_n * bn;
+  k.kb0 = k.z * p.per_slice;
+  k.n_kb = max(min(p.units, k.kb0 + p.per_slice) - k.kb0, 0);
+  return k;
+}
+// The items of a CTA: every gridDim.x-th, or (Out::stats) a run of neighbours, which lie in one row tile or a few.
+template <class S>
+__device__ __forceinline__ void term_items(int total, int& first, int& end, int& step) {
+  if constexpr (S::OUT == Out::stats) {
+    first = (int)((int64_t)total * blockIdx.x / gridDim.x);
+    end = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
+    step = 1;
+  } else {
+    first = blockIdx.x;
+    end = total;
+    step = gridDim.x;
+  }
+}
+// the CTA whose run has item i
+__host__ __device__ inline int term_owner(int i, int total, int grid) { return (int)(((int64_t)(i + 1) * grid - 1) / total); }
+
+template <class S>
+__device__ __forceinline__ void convert_b(uint8_t* terms, const uint8_t* raw, int wq, int lane, uint32_t e8) {
+  constexpr int BN = S::BN, LANES = BN / 4, LINES = 32 / LANES;  // lanes of a line of BN values, lines per instruction
+  const int n = 4 * (lane % LANES);
+#pragma unroll
+  for (int i = 0; i < 8 / LINES; ++i) {
+    const int k = wq * 8 + i * LINES + lane / LANES;
+    uint8_t* dst = terms + (n / 64) * 4096 + k * 128 + ((((n & 63) >> 3) ^ (k & 7)) << 4) + (n & 7) * 2;
+    if constexpr (S::P8) {
+      float v[4];
+      pack8_open(*reinterpret_cast<const uint32_t*>(raw + k * BN + n), v);
+      // (e8: of line wq * 8 + lane / (BN / 32), block lane % (BN / 32))
+      constexpr int EB = BN / 32;
+      const float step = pack8_step(__shfl_sync(0xffffffffu, e8, (k & 7) * EB + n / 32));
+      const uint32_t a = __byte_perm(__float_as_uint(v[0] * step), __float_as_uint(v[1] * step), 0x7632);
+      const uint32_t b = __byte_perm(__float_as_uint(v[2] * step), __float_as_uint(v[3] * step), 0x7632);
+      *reinterpret_cast<uint2*>(dst) = make_uint2(a, b);
+    } else {
+      const float4 x = *reinterpret_cast<const float4*>(raw + (n / 32) * 4096 + k * 128 + (n & 31) * 4);
+      uint2 t0, t1, t2;
+      split3(x.x, x.y, t0.x, t1.x, t2.x);
+      split3(x.z, x.w, t0.y, t1.y, t2.y);
+      *reinterpret_cast<uint2*>(dst) = t0;
+      *reinterpret_cast<uint2*>(dst + S::B_TERM) = t1;
+      *reinterpret_cast<uint2*>(dst + 2 * S::B_TERM) = t2;
+    }
+  }
+}
+
+template <class S>
+__global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_constant__ TermArgs args) {
+  constexpr int BN = S::BN, NA = S::NA, NB = S::NB, NSA = S::NSA, NSB = S::NSB, NTB = S::NTB, HALF = S::HALF;
+  constexpr bool A_TMA = S::A != ASrc::direct;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full_a = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);  // box landed
+  uint64_t* free_a = full_a + (NA ? NA : 1);                           // slot read
+  uint64_t* full_b = free_a + (NA ? NA : 1);
+  uint64_t* free_b = full_b + NB;
+  uint64_t* ready = free_b + NB;          // [NSB] terms of a k-block in place (four warps)
+  uint64_t* empty_a = ready + NSB;        // [NSA] MMAs of the stage retired
+  uint64_t* empty_b = empty_a + NSA;      // [NSB]
+  uint64_t* acc_full = empty_b + NSB;     // [2]
+  uint64_t* acc_empty = acc_full + 2;     // [2] read back by the fold warps
+  uint64_t* small_empty = acc_empty + 2;
+  uint64_t* pair = small_empty + 1;       // [4] the two fold warps of a lane quarter (Out::whole)
+  uint64_t* drain = pair + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  int* abort_slot = reinterpret_cast<int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // a wait ran out in an earlier launch or in another CTA of this one: nothing is allocated, nothing is computed
+  if (threadIdx.x == 0) *abort_slot = tc_error_now();
+  __syncthreads();
+  if (*abort_slot != 0) {
+    wait_for_predecessors();
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NA; ++i) {
+      mbar_init(&full_a[i], 1);
+      mbar_init(&free_a[i], 4);
+    }
+    for (int i = 0; i < NB; ++i) {
+      mbar_init(&full_b[i], 1);
+      mbar_init(&free_b[i], 4);
+    }
+    for (int i = 0; i < NSB; ++i) {
+      mbar_init(&ready[i], 4);
+      mbar_init(&empty_b[i], 1);
+    }
+    for (int i = 0; i < NSA; ++i) mbar_init(&empty_a[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], kFoldWarps);
+    }
+    mbar_init(small_empty, kFoldWarps);
+    for (int i = 0; i < 4; ++i) mbar_init(&pair[i], 2);
+    mbar_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(S::TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = *tmem_slot;
+  wait_for_predecessors();  // barriers and tensor memory are up; from here on global memory is read
+
+  int w0, w_end, w_step;
+  term_items<S>(args.total, w0, w_end, w_step);
+
+  if (warp < kConvWarp0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if ((warp == 0 && A_TMA) || warp == 2) {
+      // ---------------- TMA producers: warp 0 streams A, warp 2 streams B ----------------
+      if (elect_one()) {
+        const bool is_a = warp == 0;
+        const uint32_t ring = is_a ? (NA ? NA : 1) : NB;
+        uint64_t* full = is_a ? full_a : full_b;
+        uint64_t* freed = is_a ? free_a : free_b;
+        uint32_t g = 0;  // k-blocks issued so far, over all items
+        bool ok = true;
+        for (int w = w0; ok && w < w_end; w += w_step) {
+          const TermWork wk = term_work(args, w, BN);
+          const Product& p = args.p[wk.prob];
+          for (int it = 0; it < wk.n_kb; ++it, ++g) {
+            const uint32_t s = g % ring, ph = (g / ring) & 1;
+            ok = mbar_wait(&freed[s], ph ^ 1, is_a ? 41 : 42);
+            if (!ok) break;
+            const int kx = (wk.kb0 + it) * BK;
+            if (is_a) {
+              uint8_t* dst = smem + s * A_SLOT;
+              mbar_expect_tx(&full[s], A_SLOT);
+              if (S::A == ASrc::kMajor) {
+                tma_load_2d(dst, &p.map_a, kx, wk.m0, &full[s]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < BM / 32; ++j) tma_load_2d(dst + j * 4096, &p.map_a, wk.m0 + 32 * j, kx, &full[s]);
+              }
+            } else {
+              uint8_t* dst = smem + S::B_OFF + s * S::B_SLOT;
+              mbar_expect_tx(&full[s], S::B_SLOT);
+              if (S::P8) {
+                tma_load_2d(dst, &p.map_b, wk.n0, kx, &full[s]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < BN / 32; ++j) tma_load_2d(dst + j * 4096, &p.map_b, wk.n0 + 32 * j, kx, &full[s]);
+              }
+            }
+          }
+        }
+        if (!ok || tc_error_now() != 0) {  // wind down: let the copies already issued land before the CTA exits
+          const long long t0 = clock64();
+          for (uint32_t gi = g > ring ? g - ring : 0; gi < g; ++gi) {
+            const uint32_t ph = (gi / ring) & 1;
+            while (!mbar_try_wait(&full[gi % ring], ph) && clock64() - t0 < kSpinCycles) {
+            }
+          }
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer ----------------
+      // (the whole warp walks the k-blocks and one elected thread issues, so that addresses stay in uniform registers)
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(BN >> 3) << 17) | (8u << 24);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+      const uint64_t b0 = desc_b(smem_u32(smem + S::T_OFF));
+      uint32_t g = 0, folds = 0, smalls = 0;  // k-blocks, folds of the main and of the small accumulator so far
+      bool ok = true;
+      for (int w = w0; ok && w < w_end; w += w_step) {
+        const TermWork wk = term_work(args, w, BN);
+        for (int it = 0; it < wk.n_kb; ++it, ++g) {
+          const uint32_t sa = g % NSA, sb = g % NSB, pb = (g / NSB) & 1;
+          const int in_fold = it % kFoldUnits, in_small = it % (kFoldUnits * kSmallFolds);
+          if (in_fold == 0) ok = mbar_wait(&acc_empty[folds & 1], ((folds >> 1) & 1) ^ 1, 46);
+          if (ok && in_small == 0) ok = mbar_wait(small_empty, (smalls & 1) ^ 1, 47);
+          ok = ok && mbar_wait(&ready[sb], pb, 43);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const bool last_fold = in_fold == kFoldUnits - 1 || it == wk.n_kb - 1;
+          const bool last_small = in_small == kFoldUnits * kSmallFolds - 1 || it == wk.n_kb - 1;
+          const uint32_t d_main = tm + (folds & 1) * BN, d_small = tm + 2 * BN, ta = tm + S::A_COL0 + sa * S::A_COLS;
+          const uint64_t bs = b0 + (uint64_t)((sb * NTB * S::B_TERM) >> 4);
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < BK / 16; ++kk) {
+              const uint64_t bk = bs + (uint64_t)((kk * 2048) >> 4);
+              constexpr uint64_t term = S::B_TERM >> 4;
+              const uint32_t a0 = ta + 8 * kk, a1 = a0 + 16, a2 = a0 + 32;
+              // small terms first, the smallest before all
+              umma_bf16_ta(d_small, a2, bk, idesc, kk != 0 || in_small != 0);
+              if constexpr (NTB == 3) {
+                umma_bf16_ta(d_small, a0, bk + 2 * term, idesc, 1);
+                umma_bf16_ta(d_small, a1, bk + term, idesc, 1);
+                umma_bf16_ta(d_small, a0, bk + term, idesc, 1);
+              }
+              umma_bf16_ta(d_small, a1, bk, idesc, 1);
+              umma_bf16_ta(d_main, a0, bk, idesc, kk != 0 || in_fold != 0);
+            }
+            umma_commit(&empty_a[sa]);  // arrive when the MMAs above have read their operands
+            umma_commit(&empty_b[sb]);
+            if (last_fold) umma_commit(&acc_full[folds & 1]);
+          }
+          __syncwarp();
+          if (last_fold) ++folds;
+          if (last_small) ++smalls;
+        }
+      }
+      if (!ok && g > 0) {
+        // a wait ran out: the MMAs issued so far must have retired before tensor memory is given back
+        if (elect_one()) umma_commit(drain);
+        const long long t0 = clock64();
+        while (!mbar_try_wait(drain, 0) && clock64() - t0 < kSpinCycles) {
+        }
+      }
+    }
+  } else if (warp < kFoldWarp0) {
+    // ---------------- terms of the operands (warps 4..11): group 0 takes the even k-blocks, group 1 the odd ones --------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
+    const int q = warp & 3, group = (warp - kConvWarp0) >> 2, row = 32 * q + lane;  // row of the A tile
+    uint32_t g = 0;
+    bool ok = true;
+    for (int w = w0; ok && w < w_end; w += w_step) {
+      const TermWork wk = term_work(args, w, BN);
+      const Product& p = args.p[wk.prob];
+      float a_sum = 0.f;
+      const bool sums = p.a_sums != nullptr && wk.n0 == 0;
+      // steps of a packed B: a lane has the one of line q * 8 + lane / (BN / 32) of the k-block, block lane % (BN / 32) of the
+      // tile; fetched one k-block (of this group) ahead
+      uint32_t e_next = 0;
+      auto fetch_e = [&](int it) {
+        if constexpr (S::P8) {
+          constexpr int EB = BN / 32;
+          const int64_t k = (int64_t)(wk.kb0 + it) * BK + q * 8 + lane / EB;
+          const int b = wk.n0 / 32 + lane % EB;
+          e_next = it < wk.n_kb && lane < 8 * EB && k < p.k_rows && b < p.e_blocks ? p.e[k * p.lde + b] : 0u;
+        }
+      };
+      int it = (int)((group + kConvGroups - g % kConvGroups) % kConvGroups);  // first k-block of this group in the item
+      g += it;
+      fetch_e(it);
+      for (; it < wk.n_kb; it += kConvGroups, g += kConvGroups) {
+        const uint32_t sb = g % NSB, sa = g % NSA;
+        // ---- B ----
+        const uint32_t e8 = e_next;
+        fetch_e(it + kConvGroups);
+        float x[32];
+        if constexpr (!A_TMA) {  // on the way while B is split
+          const int64_t k0 = (int64_t)(wk.kb0 + it) * BK;
+          const float* src = p.a + k0 * p.lda + wk.m0 + row;
+          const bool col = wk.m0 + row < p.M;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = col && k0 + k < p.k_rows ? __ldg(src + k * p.lda) : 0.f;
+        }
+        ok = mbar_wait(&full_b[g % NB], (g / NB) & 1, 44) && mbar_wait(&empty_b[sb], ((g / NSB) & 1) ^ 1, 45);
+        ok = __all_sync(0xffffffffu, ok);  // the warp gives up as a whole
+        if (!ok) break;
+        convert_b<S>(smem + S::T_OFF + sb * NTB * S::B_TERM, smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane, e8);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&free_b[g % NB]);
+        // ---- A ----
+        uint32_t t0[16], t1[16], t2[16];
+        if constexpr (A_TMA) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&full_a[g % NA], (g / NA) & 1, 48));
+          if (!ok) break;
+          const uint8_t* slot = smem + (g % NA) * A_SLOT;
+          if constexpr (S::A == ASrc::kMajor) {
+            // 128-byte swizzle: the 16-byte chunk c of row r sits at chunk position c ^ (r % 8)
+            const uint8_t* arow = slot + (row >> 3) * 1024 + (row & 7) * 128;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const float4 v = *reinterpret_cast<const float4*>(arow + ((c ^ (row & 7)) << 4));
+              x[4 * c] = v.x; x[4 * c + 1] = v.y; x[4 * c + 2] = v.z; x[4 * c + 3] = v.w;
+            }
+          } else {
+            const uint8_t* s = slot + q * 4096 + lane * 4;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] = *reinterpret_cast<const float*>(s + k * 128);
+          }
+        }
+        if (sums) {
+          float s8[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s8[k] = (x[k] + x[k + 8]) + (x[k + 16] + x[k + 24]);
+          a_sum += ((s8[0] + s8[1]) + (s8[2] + s8[3])) + ((s8[4] + s8[5]) + (s8[6] + s8[7]));
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) split3(x[2 * k], x[2 * k + 1], t0[k], t1[k], t2[k]);
+        if constexpr (A_TMA) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&free_a[g % NA]);
+        }
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty_a[sa], ((g / NSA) & 1) ^ 1, 49));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t ta = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(S::A_COL0 + sa * S::A_COLS);
+        tmem_st16(ta, t0);
+        tmem_st16(ta + 16, t1);
+        tmem_st16(ta + 32, t2);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the MMA
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ready[sb]);
+      }
+      if (!ok) break;
+      g -= it - wk.n_kb;  // k-blocks of both groups
+      if (sums && wk.m0 + row < p.M) p.a_sums[(2 * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
+    }
+  } else {
+    // ---------------- folds and results (warps 12..19) ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsFold));
+    const int quad = warp & 3, half = (warp - kFoldWarp0) >> 2;
+    const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + half * HALF;
+    uint32_t folds = 0;
+    float run_m = -INFINITY, run_s = 0.f;  // (Out::stats)
+    uint32_t met = 0;                      // (Out::whole) meetings of the two warps of a quarter
+    bool ok = true;
+    auto meet = [&]() {  // what either wrote to shared memory before is there for the other one; false: a wait ran out
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&pair[quad]);
+      const bool there = __all_sync(0xffffffffu, mbar_wait(&pair[quad], met & 1, 51));
+      ++met;
+      return there;
+    };
+    for (int w = w0; ok && w < w_end; w += w_step) {
+      const TermWork wk = term_work(args, w, BN);
+      const Product& p = args.p[wk.prob];
+      const int m = wk.m0 + quad * 32 + lane, nb = wk.n0 + half * HALF;
+      const bool row_in = m < p.M;
+      // what the epilogue needs of its row, on the way while the sums are made
+      int label = -1;
+      float lse = 0.f;
+      bool on = row_in;
+      if constexpr (S::OUT != Out::transposed) {
+        if (row_in) label = max(__ldg(args.ce.y + m), -1);
+        if constexpr (S::OUT == Out::grad)
+          if (row_in) lse = __ldg(args.ce.lse + m);
+        if constexpr (S::OUT == Out::whole) on = row_in && (!args.ce.mask || __ldg(args.ce.mask + m) != 0);
+      }
+      float sum[HALF];
+#pragma unroll
+      for (int j = 0; j < HALF; ++j) sum[j] = 0.f;
+      for (int it = 0; it < wk.n_kb; it += kFoldUnits, ++folds) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[folds & 1], (folds >> 1) & 1, 50));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int done = it + kFoldUnits;
+        const bool small = done >= wk.n_kb || done % (kFoldUnits * kSmallFolds) == 0;
+#pragma unroll
+        for (int c0 = 0; c0 < HALF; c0 += 32) {
+          uint32_t v[32];
+          tmem_ld32(lanes + (folds & 1) * BN + c0, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[c0 + j] += __uint_as_float(v[j]);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&acc_empty[folds & 1]);
+        if (small) {
+#pragma unroll
+          for (int c0 = 0; c0 < HALF; c0 += 32) {
+            uint32_t v[32];
+            tmem_ld32(lanes + 2 * BN + c0, v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[c0 + j] += __uint_as_float(v[j]);
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(small_empty);
+        }
+      }
+      if (!ok) break;
+      if constexpr (S::OUT == Out::transposed) {
+        if (p.write && m < p.m_pad) {
+          float* dst = p.c + wk.z * p.slice_stride + m;
+#pragma unroll
+          for (int j = 0; j < HALF; ++j) {
+            if (nb + j >= p.N) break;
+            const int64_t r = p.row_map ? __ldg(p.row_map + nb + j) : nb + j;
+            if (r < 0) continue;
+            float* at = dst + r * p.ldc;
+            *at = p.accumulate ? *at + sum[j] : sum[j];
+          }
+        }
+      } else {
+        const int cols = min(HALF, p.N - nb);  // classes of this half (may be below 1)
+        const int c0 = args.ce.c0 + nb;
+        if (args.ce.bias) {
+#pragma unroll
+          for (int j = 0; j < HALF; ++j)
+            if (j < cols) sum[j] += __ldg(args.ce.bias + c0 + j);
+        }
+        label -= c0;  // relative to this half
+        if constexpr (S::OUT == Out::grad) {
+          float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
+          if (row_in)
+#pragma unroll
+            for (int j = 0; j < HALF; ++j)
+              if (j < cols) gt[(int64_t)j * args.ce.ldg] = (expf(sum[j] - lse) - (j == label ? 1.f : 0.f)) * args.ce.inv_nt;
+        } else {
+          float mx = -INFINITY, zy = 0.f;
+#pragma unroll
+          for (int j = 0; j < HALF; ++j)
+            if (j < cols) {
+              mx = fmaxf(mx, sum[j]);
+              if (j == label) zy = sum[j];
+            }
+          const bool here = label >= 0 && label < cols;
+          if constexpr (S::OUT == Out::stats) {
+            if (here && row_in) args.ce.zy[m] = zy;
+            // the run's maximum and sum go on; a maximum of -infinity has nothing to be subtracted from
+            const float top = fmaxf(run_m, mx), base = top == -INFINITY ? 0.f : top;
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < HALF; ++j)
+              if (j < cols) s += expf(sum[j] - base);
+            run_s = run_s * expf(run_m - base) + s;
+            run_m = top;
+            const int next = w + 1;
+            if (next >= w_end || next / p.tiles_n != w / p.tiles_n) {
+              const int64_t slot = ((int64_t)(blockIdx.x + w / p.tiles_n) * 2 + half) * BM + quad * 32 + lane;
+              args.ce.part_m[slot] = run_m;
+              args.ce.part_s[slot] = run_s;
+              run_m = -INFINITY;
+              run_s = 0.f;
+            }
+          } else {
+            // both halves of a row: maxima, then sums and the label's logit, through shared memory
+            float* xm = reinterpret_cast<float*>(smem + S::X_OFF);
+            float* xs = xm + 2 * BM;
+            const int r = quad * 32 + lane;
+            xm[half * BM + r] = mx;
+            ok = meet();
+            if (!ok) break;
+            const float top = fmaxf(xm[r], xm[BM + r]), base = top == -INFINITY ? 0.f : top;
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) {
+              sum[j] = j < cols ? expf(sum[j] - base) : 0.f;
+              s += sum[j];
+            }
+            xs[half * BM + r] = s;
+            ok = meet();
+            if (!ok) break;
+            s = xs[r] + xs[BM + r];
+            if (row_in) {
+              const float inv = 1.f / s;
+              if (here || (half == 0 && (label + c0 < 0 || label + c0 >= p.N)))  // (a label outside: no logit)
+                args.ce.row_loss[m] = !on ? 0.f : here ? (base + logf(s)) - zy : NAN;
+              if (args.ce.gt) {
+                float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
+#pragma unroll
+                for (int j = 0; j < HALF; ++j)
+                  if (j < cols) gt[(int64_t)j * args.ce.ldg] = on ? (sum[j] * inv - (j == label ? 1.f : 0.f)) * args.ce.inv_nt : 0.f;
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(S::TMEM_COLS) : "memory");
+  }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------------
+// fp32 matrix with `inner` contiguous elements per line and `outer` lines, pitch ld; zero fill outside.  K-major: boxes of 32 k
+// x `box_outer` lines, 128-byte swizzle; MN-major: boxes of 32 x 32 as they are.
+inline bool term_map(CUtensorMap* map, const void* base, bool bytes, int64_t outer, int64_t inner, int64_t ld, int box_inner, int box_outer, bool swizzle) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * (bytes ? 1 : sizeof(float))};
+  cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, (void*)base, dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class S>
+cudaError_t run_terms(cudaStream_t s, const TermArgs& a, int grid) {
+  cudaError_t e = cudaFuncSetAttribute(term_product<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  return launch(term_product<S>, grid, kTermThreads, S::SMEM_BYTES, s, a);
+}
+
+}  // namespace
+}  // namespace gcnsa
