@@ -1,18 +1,18 @@
 // D = A B on the 5th-generation tensor cores from bf16 terms, with sums that keep fp32 accuracy however long they are.
 //
 // A fp32 value is the exact sum of three bf16 terms (24 significant bits cut into 8 + 8 + 8); of the nine products of two
-// such operands the three smallest lie below 2^-22 of the product and are left out.  An operand that is an 8-bit checkpoint
+// such operands the three smallest are left out (each below 2^-21 of the product, about 2^-24 on average).  An operand that is an 8-bit checkpoint
 // is one bf16 term.  The tensor core cuts a sum off at 24 bits, always toward zero, where an fp32 addition rounds, so an
 // accumulator may not live long: the products of the leading terms go into one of two accumulators in turn, two
-// instructions per 32 k, and after kFoldUnits x 32 k its sum is added to running sums in registers (rounded), while the
+// instructions per 32 k, and after 256 k its sum is added to running sums in registers (rounded), while the
 // MMAs go on in the other one.  The products of the smaller terms have a third accumulator; what is cut off there is
 // 2^-8 of that, and it is folded every kSmallFolds folds.  (One accumulator for everything over 245 000 rows would be
 // 1e-4 off.)
 //
 // One CTA per SM works on tiles of 128 x BN.  Warps 0 and 2 stream boxes of A and B into rings of shared memory with TMA;
-// two groups of four warps (4-11) take every other k-block each: A goes as three terms into tensor memory (a lane per row
+// three groups of four warps (4-15) take every third k-block each: A goes as three terms into tensor memory (a lane per row
 // of the tile, two k per 32-bit column), B as one or three terms into MN-major tiles with the 128-byte swizzle.  Warp 1
-// issues the MMAs, and eight warps (12-19, two per lane quarter of tensor memory, half the columns each) fold the
+// issues the MMAs, and eight warps (16-23, two per lane quarter of tensor memory, half the columns each) fold the
 // accumulators and write the result: thread = row of the tile, so a result that is wanted transposed, D[m, n] at
 // c[n * ldc + m], is written in lines of 128 bytes without a turn through shared memory.  Every product of this file is
 // arranged so that this is the layout it needs.
@@ -35,11 +35,11 @@ namespace gcnsa {
 namespace {
 
 constexpr int BM = 128, BK = 32;
-constexpr int kConvWarp0 = 4, kConvGroups = 2, kFoldWarp0 = 12, kFoldWarps = 8, kTermThreads = 32 * (kFoldWarp0 + kFoldWarps);
-// registers per thread by role, in multiples of 8; their sum over the five warpgroups is what the launch gives (96 each)
-constexpr int kRegsIssue = 48, kRegsConv = 80, kRegsFold = 136;
-static_assert(kRegsIssue + 2 * kRegsConv + 2 * kRegsFold <= 5 * 96, "setmaxnreg draws on the registers of the launch");
-constexpr int kFoldUnits = 8, kSmallFolds = 8;
+constexpr int kConvWarp0 = 4, kConvGroups = 3, kFoldWarp0 = 16, kFoldWarps = 8, kTermThreads = 32 * (kFoldWarp0 + kFoldWarps);
+// registers per thread by role, in multiples of 8; their sum over the six warpgroups is at most what the launch gives (80 each)
+constexpr int kRegsIssue = 40, kRegsConv = 80, kRegsFold = 96;
+static_assert(kRegsIssue + kConvGroups * kRegsConv + 2 * kRegsFold <= 6 * 80, "setmaxnreg draws on the registers of the launch");
+constexpr int kSmallFolds = 8;
 constexpr int A_SLOT = BM * BK * 4;
 
 // A: K-major (k contiguous in memory), MN-major (rows of D contiguous), or MN-major without the alignment that TMA needs
@@ -55,7 +55,7 @@ struct Product {
   int64_t ldc, slice_stride;
   const int32_t* row_map;  // row(n), nullable; negative: not written
   int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros
-  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of parity g: a_sums[(2 z + g) * sums_pitch + m]
+  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(kConvGroups z + g) * sums_pitch + m]
   int64_t sums_pitch;
   int write;               // 0: only a_sums are wanted
   const float* a;          // ASrc::direct
@@ -118,17 +118,28 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
-// Two values as three pairs of bf16 terms, the first value in the lower halves.  The leading term is cut off, so that no
-// finite value becomes an infinity; what is left of it is exact, the second term is rounded, and the third holds the rest
-// exactly.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// Two values as three pairs of bf16 terms, the first value in the lower halves.  Every term is what its upper 16 bits say (cut
+// off, not rounded: no finite value becomes an infinity, and a byte permute packs two of them, where cvt.rn.bf16x2 has a
+// fraction of that rate); 8 + 8 + 8 bits are all that a value has.
 __device__ __forceinline__ void split3(float x0, float x1, uint32_t& t0, uint32_t& t1, uint32_t& t2) {
-  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(t0) : "f"(x1), "f"(x0));
-  x0 -= __uint_as_float(t0 << 16);
-  x1 -= __uint_as_float(t0 & 0xffff0000u);
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(t1) : "f"(x1), "f"(x0));
-  x0 -= __uint_as_float(t1 << 16);
-  x1 -= __uint_as_float(t1 & 0xffff0000u);
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(t2) : "f"(x1), "f"(x0));
+  auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); };
+  t0 = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+  x0 -= upper(x0);
+  x1 -= upper(x1);
+  t1 = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+  x0 -= upper(x0);
+  x1 -= upper(x1);
+  t2 = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
 }
 
 template <int BN_, ASrc A_, bool P8_, Out OUT_>
@@ -139,17 +150,26 @@ struct TermShape {
   static constexpr Out OUT = OUT_;
   static constexpr int NTB = P8 ? 1 : 3;                 // terms of B
   static constexpr int HALF = BN / 2;                    // columns of a fold warp
-  static constexpr int A_COLS = 48;                      // tensor-memory columns of a stage of A
-  static constexpr int NSA = BN == 64 ? 4 : 2, NSB = 3;  // stages of terms
-  static constexpr int A_COL0 = 3 * BN, TMEM_COLS = 512;
+  // With one term of B all three products of a k-block share an accumulator, which is folded twice as often; the columns of
+  // the third one hold more stages of A.
+  static constexpr bool SMALL = !P8;
+  static constexpr int FOLD = SMALL ? 8 : 4;             // k-blocks to a fold
+  static constexpr int A_COLS = 48, A_COL0 = (SMALL ? 3 : 2) * BN, TMEM_COLS = 512;  // tensor-memory columns
+  static constexpr int NSA = (TMEM_COLS - A_COL0) / A_COLS < 5 ? (TMEM_COLS - A_COL0) / A_COLS : 5, NSB = P8 ? 6 : 3;  // stages of terms
   static constexpr int B_SLOT = BK * BN * (P8 ? 1 : 4), B_TERM = BK * BN * 2;
-  static constexpr int NA = A == ASrc::direct ? 0 : 4, NB = P8 ? 8 : 4;  // landing slots
+  // Landing slots, a multiple of the groups: a slot's boxes are then all read by one group, in order.  (A wait by parity cannot
+  // tell a phase from the one two before it, and boxes land out of order: with four slots a group could take a slot whose
+  // box before the last was still on its way for one that had landed.)
+  static constexpr int NA = A == ASrc::direct ? 0 : 6, NB = P8 ? 6 : 3;
   static constexpr int B_OFF = NA * A_SLOT, T_OFF = B_OFF + NB * B_SLOT, X_OFF = T_OFF + NSB * NTB * B_TERM;
   static constexpr int X_BYTES = OUT == Out::whole ? 2 * 2 * BM * 4 : 0;  // maxima and sums of the halves of a row
   static constexpr int BAR_OFF = X_OFF + X_BYTES;
   // more than half of an SM's shared memory: a second CTA, which would wait for tensor memory, never shares the SM
   static constexpr int NEED = BAR_OFF + 512 + 1024;
   static constexpr int SMEM_BYTES = NEED > 118 * 1024 ? NEED : 118 * 1024;
+  static_assert(NA % kConvGroups == 0 && NB % kConvGroups == 0 && NSB % kConvGroups == 0, "a slot belongs to one group");
+  // stages of A are not: a group that waits for stage g % NSA has seen the MMAs of k-block g - NSB retire
+  static_assert(NSB <= 2 * NSA, "the phase before the last of a stage of A has ended");
   static_assert(A_COL0 + NSA * A_COLS <= TMEM_COLS, "tensor memory has 512 columns");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
 };
@@ -187,41 +207,58 @@ __device__ __forceinline__ void term_items(int total, int& first, int& end, int&
 // the CTA whose run has item i
 __host__ __device__ inline int term_owner(int i, int total, int grid) { return (int)(((int64_t)(i + 1) * grid - 1) / total); }
 
+// A group's k-block of B: a lane has four neighbouring n of line(i), i below COUNT.  Loaded as a whole before the first term
+// is written: the compiler cannot tell that the boxes and the terms do not overlap, and line by line every load would wait for the
+// stores before it (1 370 clocks a k-block instead of 520).
 template <class S>
-__device__ __forceinline__ void convert_b(uint8_t* terms, const uint8_t* raw, int wq, int lane, uint32_t e8) {
-  constexpr int BN = S::BN, LANES = BN / 4, LINES = 32 / LANES;  // lanes of a line of BN values, lines per instruction
-  const int n = 4 * (lane % LANES);
+struct TermB {
+  static constexpr int LANES = S::BN / 4, LINES = 32 / LANES, COUNT = 8 / LINES;  // lanes of a line, lines per instruction
+  float4 x[S::P8 ? 1 : COUNT];
+  uint32_t q[S::P8 ? COUNT : 1];
+  static __device__ __forceinline__ int line(int i, int wq, int lane) { return wq * 8 + i * LINES + lane / LANES; }
+  __device__ __forceinline__ void load(const uint8_t* raw, int wq, int lane) {
+    const int n = 4 * (lane % LANES);
 #pragma unroll
-  for (int i = 0; i < 8 / LINES; ++i) {
-    const int k = wq * 8 + i * LINES + lane / LANES;
-    uint8_t* dst = terms + (n / 64) * 4096 + k * 128 + ((((n & 63) >> 3) ^ (k & 7)) << 4) + (n & 7) * 2;
-    if constexpr (S::P8) {
-      float v[4];
-      pack8_open(*reinterpret_cast<const uint32_t*>(raw + k * BN + n), v);
-      // (e8: of line wq * 8 + lane / (BN / 32), block lane % (BN / 32))
-      constexpr int EB = BN / 32;
-      const float step = pack8_step(__shfl_sync(0xffffffffu, e8, (k & 7) * EB + n / 32));
-      const uint32_t a = __byte_perm(__float_as_uint(v[0] * step), __float_as_uint(v[1] * step), 0x7632);
-      const uint32_t b = __byte_perm(__float_as_uint(v[2] * step), __float_as_uint(v[3] * step), 0x7632);
-      *reinterpret_cast<uint2*>(dst) = make_uint2(a, b);
-    } else {
-      const float4 x = *reinterpret_cast<const float4*>(raw + (n / 32) * 4096 + k * 128 + (n & 31) * 4);
-      uint2 t0, t1, t2;
-      split3(x.x, x.y, t0.x, t1.x, t2.x);
-      split3(x.z, x.w, t0.y, t1.y, t2.y);
-      *reinterpret_cast<uint2*>(dst) = t0;
-      *reinterpret_cast<uint2*>(dst + S::B_TERM) = t1;
-      *reinterpret_cast<uint2*>(dst + 2 * S::B_TERM) = t2;
+    for (int i = 0; i < COUNT; ++i) {
+      const int k = line(i, wq, lane);
+      if constexpr (S::P8) q[i] = *reinterpret_cast<const uint32_t*>(raw + k * S::BN + n);
+      else x[i] = *reinterpret_cast<const float4*>(raw + (n / 32) * 4096 + k * 128 + (n & 31) * 4);
     }
   }
-}
+  // e8: the step of line wq * 8 + lane / (BN / 32), block lane % (BN / 32) of a packed B
+  __device__ __forceinline__ void store(uint8_t* terms, int wq, int lane, uint32_t e8) const {
+    const int n = 4 * (lane % LANES);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      const int k = line(i, wq, lane);
+      uint8_t* dst = terms + (n / 64) * 4096 + k * 128 + ((((n & 63) >> 3) ^ (k & 7)) << 4) + (n & 7) * 2;
+      if constexpr (S::P8) {
+        float v[4];
+        pack8_open(q[i], v);
+        constexpr int EB = S::BN / 32;
+        const float step = pack8_step(__shfl_sync(0xffffffffu, e8, (k & 7) * EB + n / 32));
+        const uint32_t a = __byte_perm(__float_as_uint(v[0] * step), __float_as_uint(v[1] * step), 0x7632);
+        const uint32_t b = __byte_perm(__float_as_uint(v[2] * step), __float_as_uint(v[3] * step), 0x7632);
+        *reinterpret_cast<uint2*>(dst) = make_uint2(a, b);
+      } else {
+        uint2 t0, t1, t2;
+        split3(x[i].x, x[i].y, t0.x, t1.x, t2.x);
+        split3(x[i].z, x[i].w, t0.y, t1.y, t2.y);
+        *reinterpret_cast<uint2*>(dst) = t0;
+        *reinterpret_cast<uint2*>(dst + S::B_TERM) = t1;
+        *reinterpret_cast<uint2*>(dst + 2 * S::B_TERM) = t2;
+      }
+    }
+  }
+};
 
 template <class S>
 __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_constant__ TermArgs args) {
   constexpr int BN = S::BN, NA = S::NA, NB = S::NB, NSA = S::NSA, NSB = S::NSB, NTB = S::NTB, HALF = S::HALF;
   constexpr bool A_TMA = S::A != ASrc::direct;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  // (an offset, not a rounded pointer: the compiler then knows that this is shared memory and need not use generic accesses)
+  uint8_t* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint64_t* full_a = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);  // box landed
   uint64_t* free_a = full_a + (NA ? NA : 1);                           // slot read
   uint64_t* full_b = free_a + (NA ? NA : 1);
@@ -344,16 +381,16 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         const TermWork wk = term_work(args, w, BN);
         for (int it = 0; it < wk.n_kb; ++it, ++g) {
           const uint32_t sa = g % NSA, sb = g % NSB, pb = (g / NSB) & 1;
-          const int in_fold = it % kFoldUnits, in_small = it % (kFoldUnits * kSmallFolds);
+          const int in_fold = it % S::FOLD, in_small = it % (S::FOLD * kSmallFolds);
           if (in_fold == 0) ok = mbar_wait(&acc_empty[folds & 1], ((folds >> 1) & 1) ^ 1, 46);
-          if (ok && in_small == 0) ok = mbar_wait(small_empty, (smalls & 1) ^ 1, 47);
+          if (S::SMALL && ok && in_small == 0) ok = mbar_wait(small_empty, (smalls & 1) ^ 1, 47);
           ok = ok && mbar_wait(&ready[sb], pb, 43);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const bool last_fold = in_fold == kFoldUnits - 1 || it == wk.n_kb - 1;
-          const bool last_small = in_small == kFoldUnits * kSmallFolds - 1 || it == wk.n_kb - 1;
-          const uint32_t d_main = tm + (folds & 1) * BN, d_small = tm + 2 * BN, ta = tm + S::A_COL0 + sa * S::A_COLS;
+          const bool last_fold = in_fold == S::FOLD - 1 || it == wk.n_kb - 1;
+          const bool last_small = in_small == S::FOLD * kSmallFolds - 1 || it == wk.n_kb - 1;
+          const uint32_t d_main = tm + (folds & 1) * BN, d_small = S::SMALL ? tm + 2 * BN : d_main, ta = tm + S::A_COL0 + sa * S::A_COLS;
           const uint64_t bs = b0 + (uint64_t)((sb * NTB * S::B_TERM) >> 4);
           if (elect_one()) {
 #pragma unroll
@@ -362,14 +399,14 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
               constexpr uint64_t term = S::B_TERM >> 4;
               const uint32_t a0 = ta + 8 * kk, a1 = a0 + 16, a2 = a0 + 32;
               // small terms first, the smallest before all
-              umma_bf16_ta(d_small, a2, bk, idesc, kk != 0 || in_small != 0);
+              umma_bf16_ta(d_small, a2, bk, idesc, kk != 0 || (S::SMALL ? in_small : in_fold) != 0);
               if constexpr (NTB == 3) {
                 umma_bf16_ta(d_small, a0, bk + 2 * term, idesc, 1);
                 umma_bf16_ta(d_small, a1, bk + term, idesc, 1);
                 umma_bf16_ta(d_small, a0, bk + term, idesc, 1);
               }
               umma_bf16_ta(d_small, a1, bk, idesc, 1);
-              umma_bf16_ta(d_main, a0, bk, idesc, kk != 0 || in_fold != 0);
+              umma_bf16_ta(d_main, a0, bk, idesc, !S::SMALL || kk != 0 || in_fold != 0);
             }
             umma_commit(&empty_a[sa]);  // arrive when the MMAs above have read their operands
             umma_commit(&empty_b[sb]);
@@ -389,7 +426,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       }
     }
   } else if (warp < kFoldWarp0) {
-    // ---------------- terms of the operands (warps 4..11): group 0 takes the even k-blocks, group 1 the odd ones --------
+    // ---------------- terms of the operands (warps 4..15): every third k-block to a group ----------------
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
     const int q = warp & 3, group = (warp - kConvWarp0) >> 2, row = 32 * q + lane;  // row of the A tile
     uint32_t g = 0;
@@ -426,11 +463,16 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
 #pragma unroll
           for (int k = 0; k < 32; ++k) x[k] = col && k0 + k < p.k_rows ? __ldg(src + k * p.lda) : 0.f;
         }
-        ok = mbar_wait(&full_b[g % NB], (g / NB) & 1, 44) && mbar_wait(&empty_b[sb], ((g / NSB) & 1) ^ 1, 45);
-        ok = __all_sync(0xffffffffu, ok);  // the warp gives up as a whole
+        ok = __all_sync(0xffffffffu, mbar_wait(&full_b[g % NB], (g / NB) & 1, 44));  // the warp gives up as a whole
         if (!ok) break;
-        convert_b<S>(smem + S::T_OFF + sb * NTB * S::B_TERM, smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane, e8);
+        TermB<S> tb;
+        tb.load(smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane);
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty_b[sb], ((g / NSB) & 1) ^ 1, 45));
+        if (!ok) break;
+        tb.store(smem + S::T_OFF + sb * NTB * S::B_TERM, q, lane, e8);
         __syncwarp();
+        // A slot is given back when what was made of it has been stored, not when it has been loaded: nothing keeps the loads
+        // themselves in front of the arrival (with it straight behind them results changed from run to run).
         if (lane == 0) mbar_arrive(&free_b[g % NB]);
         // ---- A ----
         uint32_t t0[16], t1[16], t2[16];
@@ -460,10 +502,6 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         }
 #pragma unroll
         for (int k = 0; k < 16; ++k) split3(x[2 * k], x[2 * k + 1], t0[k], t1[k], t2[k]);
-        if constexpr (A_TMA) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&free_a[g % NA]);
-        }
         ok = __all_sync(0xffffffffu, mbar_wait(&empty_a[sa], ((g / NSA) & 1) ^ 1, 49));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -471,6 +509,10 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         tmem_st16(ta, t0);
         tmem_st16(ta + 16, t1);
         tmem_st16(ta + 32, t2);
+        if constexpr (A_TMA) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&free_a[g % NA]);
+        }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the MMA
@@ -478,11 +520,11 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         if (lane == 0) mbar_arrive(&ready[sb]);
       }
       if (!ok) break;
-      g -= it - wk.n_kb;  // k-blocks of both groups
-      if (sums && wk.m0 + row < p.M) p.a_sums[(2 * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
+      g -= it - wk.n_kb;  // k-blocks of all groups
+      if (sums && wk.m0 + row < p.M) p.a_sums[(kConvGroups * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
     }
   } else {
-    // ---------------- folds and results (warps 12..19) ----------------
+    // ---------------- folds and results (warps 16..23) ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsFold));
     const int quad = warp & 3, half = (warp - kFoldWarp0) >> 2;
     const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + half * HALF;
@@ -515,30 +557,27 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       float sum[HALF];
 #pragma unroll
       for (int j = 0; j < HALF; ++j) sum[j] = 0.f;
-      for (int it = 0; it < wk.n_kb; it += kFoldUnits, ++folds) {
+      for (int it = 0; it < wk.n_kb; it += S::FOLD, ++folds) {
         ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[folds & 1], (folds >> 1) & 1, 50));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const int done = it + kFoldUnits;
-        const bool small = done >= wk.n_kb || done % (kFoldUnits * kSmallFolds) == 0;
+        const int done = it + S::FOLD;
+        const bool small = S::SMALL && (done >= wk.n_kb || done % (S::FOLD * kSmallFolds) == 0);
+        auto fold = [&](uint32_t acc) {
 #pragma unroll
-        for (int c0 = 0; c0 < HALF; c0 += 32) {
-          uint32_t v[32];
-          tmem_ld32(lanes + (folds & 1) * BN + c0, v);
+          for (int c0 = 0; c0 < HALF; c0 += 16) {
+            uint32_t v[16];
+            tmem_ld16(acc + c0, v);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) sum[c0 + j] += __uint_as_float(v[j]);
-        }
+            for (int j = 0; j < 16; ++j) sum[c0 + j] += __uint_as_float(v[j]);
+          }
+        };
+        fold(lanes + (folds & 1) * BN);
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(&acc_empty[folds & 1]);
         if (small) {
-#pragma unroll
-          for (int c0 = 0; c0 < HALF; c0 += 32) {
-            uint32_t v[32];
-            tmem_ld32(lanes + 2 * BN + c0, v);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) sum[c0 + j] += __uint_as_float(v[j]);
-          }
+          fold(lanes + 2 * BN);
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(small_empty);
