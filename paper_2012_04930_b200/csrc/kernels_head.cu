@@ -231,7 +231,7 @@ CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   p.gt_floats = whole ? c * n4 : std::min(c128 * n4, std::max(kPieceFloats, 128 * n4));
   // at most 2 x SMs items of slices of dW^T (pick_slices)
   p.partial_floats = n > 0 ? std::min(2 * sms, std::max<int64_t>(div_up(n, BK), 1) * div_up(d, 128) * (c128 / 128)) * 128 * 128 : 0;
-  p.sums_floats = n > 0 ? kConvGroups * std::max<int64_t>(2 * sms * 128, c128) : 0;  // a line per slice and group
+  p.sums_floats = n > 0 ? kSplitGroups * std::max<int64_t>(2 * sms * 128, c128) : 0;  // a line per slice and group
   p.slots = sms + div_up(n, BM);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += up256(bytes); return o; };
@@ -475,7 +475,7 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     if (a.dw && slices > 1)
       GCNSA_STEP(launch_splitk_reduce(stream, a.d, width, slices, (const float*)f_at(pl.partial), up4(width), a.dw + c0, a.lddw, a.accumulate, GCNSA_EPI_NONE, nullptr, 0));
     if (a.db) {
-      GCNSA_STEP(launch(sum_lines, (int)div_up(width, 256), 256, 0, s, (int)width, kConvGroups * slices, (const float*)f_at(pl.sums), up4(width), a.db + c0, a.accumulate));
+      GCNSA_STEP(launch(sum_lines, (int)div_up(width, 256), 256, 0, s, (int)width, kSplitGroups * slices, (const float*)f_at(pl.sums), up4(width), a.db + c0, a.accumulate));
       note_launch();
     }
   }

@@ -9,13 +9,14 @@
 // 2^-8 of that, and it is folded every kSmallFolds folds.  (One accumulator for everything over 245 000 rows would be
 // 1e-4 off.)
 //
-// One CTA per SM works on tiles of 128 x BN.  Warps 0 and 2 stream boxes of A and B into rings of shared memory with TMA;
-// three groups of four warps (4-15) take every third k-block each: A goes as three terms into tensor memory (a lane per row
-// of the tile, two k per 32-bit column), B as one or three terms into MN-major tiles with the 128-byte swizzle.  Warp 1
-// issues the MMAs, and eight warps (16-23, two per lane quarter of tensor memory, half the columns each) fold the
-// accumulators and write the result: thread = row of the tile, so a result that is wanted transposed, D[m, n] at
-// c[n * ldc + m], is written in lines of 128 bytes without a turn through shared memory.  Every product of this file is
-// arranged so that this is the layout it needs.
+// One CTA per SM works on tiles of 128 x BN.  Warps 0 and 2 stream boxes of A and B into rings of shared memory with TMA.
+// Two groups of four warps (4-11) take every other k-block of A and leave it as three terms in tensor memory (a lane per row of
+// the tile, two k per 32-bit column), two more groups (12-19) every other k-block of B, as one or three terms in MN-major
+// tiles with the 128-byte swizzle.  (With both operands of a k-block in one group's hands, a stage that the MMAs had
+// given back stood empty for 1 700 clocks.)  Warp 1 issues the MMAs, and eight warps (20-27, two per lane quarter of tensor
+// memory, half the columns each) fold the accumulators and write the result: thread = row of the tile, so a result that is
+// wanted transposed, D[m, n] at c[n * ldc + m], is written in lines of 128 bytes without a turn through shared memory.
+// Every product of this file is arranged so that this is the layout it needs.
 //
 // A k-block of 32 of a 128 x 128 tile keeps the tensor pipe busy for 768 clocks (12 MMAs) and shared memory for about
 // 1 090 (boxes in 256, both read for the split 256, terms of B out 192, B read by the MMAs 384, at 128 bytes a clock): the
@@ -35,10 +36,10 @@ namespace gcnsa {
 namespace {
 
 constexpr int BM = 128, BK = 32;
-constexpr int kConvWarp0 = 4, kConvGroups = 3, kFoldWarp0 = 16, kFoldWarps = 8, kTermThreads = 32 * (kFoldWarp0 + kFoldWarps);
-// registers per thread by role, in multiples of 8; their sum over the six warpgroups is at most what the launch gives (80 each)
-constexpr int kRegsIssue = 40, kRegsConv = 80, kRegsFold = 96;
-static_assert(kRegsIssue + kConvGroups * kRegsConv + 2 * kRegsFold <= 6 * 80, "setmaxnreg draws on the registers of the launch");
+constexpr int kAWarp0 = 4, kBWarp0 = 12, kSplitGroups = 2, kFoldWarp0 = 20, kFoldWarps = 8, kTermThreads = 32 * (kFoldWarp0 + kFoldWarps);
+// registers per thread by role, in multiples of 8; their sum over the seven warpgroups is at most what the launch gives (72 each)
+constexpr int kRegsIssue = 32, kRegsA = 72, kRegsB = 64, kRegsFold = 96;
+static_assert(kRegsIssue + kSplitGroups * (kRegsA + kRegsB) + 2 * kRegsFold <= 7 * 72, "setmaxnreg draws on the registers of the launch");
 constexpr int kSmallFolds = 8;
 constexpr int A_SLOT = BM * BK * 4;
 
@@ -55,7 +56,7 @@ struct Product {
   int64_t ldc, slice_stride;
   const int32_t* row_map;  // row(n), nullable; negative: not written
   int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros
-  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(kConvGroups z + g) * sums_pitch + m]
+  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(kSplitGroups z + g) * sums_pitch + m]
   int64_t sums_pitch;
   int write;               // 0: only a_sums are wanted
   const float* a;          // ASrc::direct
@@ -128,6 +129,37 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
       : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
+// Bounded wait as mbar_wait, for phases that last microseconds: the thread asks to be put aside for up to 2 us at a time, as 12
+// warps that poll take a third of the issue slots from those that split and fold.
+__device__ __forceinline__ bool mbar_wait_long(uint64_t* bar, uint32_t parity, int code) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  for (;;) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        " .reg .pred p;\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 2000;\n"
+        " selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if (tc_error_now() != 0) return false;
+    if (clock64() - t0 > kSpinCycles) {
+      atomicCAS(&g_tc_error, 0, code);
+      return false;
+    }
+  }
+}
+// 2^x (2 units in the last place; 0 for -infinity, NaN for NaN)
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2e = 1.44269504088896340736f;
 // Two values as three pairs of bf16 terms, the first value in the lower halves.  Every term is what its upper 16 bits say (cut
 // off, not rounded: no finite value becomes an infinity, and a byte permute packs two of them, where cvt.rn.bf16x2 has a
 // fraction of that rate); 8 + 8 + 8 bits are all that a value has.
@@ -158,18 +190,20 @@ struct TermShape {
   static constexpr int NSA = (TMEM_COLS - A_COL0) / A_COLS < 5 ? (TMEM_COLS - A_COL0) / A_COLS : 5, NSB = P8 ? 6 : 3;  // stages of terms
   static constexpr int B_SLOT = BK * BN * (P8 ? 1 : 4), B_TERM = BK * BN * 2;
   // Landing slots, a multiple of the groups: a slot's boxes are then all read by one group, in order.  (A wait by parity cannot
-  // tell a phase from the one two before it, and boxes land out of order: with four slots a group could take a slot whose
-  // box before the last was still on its way for one that had landed.)
-  static constexpr int NA = A == ASrc::direct ? 0 : 6, NB = P8 ? 6 : 3;
+  // tell a phase from the one two before it, and boxes land out of order: with four slots and three groups a group could
+  // take a slot whose box before the last was still on its way for one that had landed.)
+  static constexpr int NA = A == ASrc::direct ? 0 : P8 ? 6 : 4, NB = P8 ? 6 : 4;
   static constexpr int B_OFF = NA * A_SLOT, T_OFF = B_OFF + NB * B_SLOT, X_OFF = T_OFF + NSB * NTB * B_TERM;
-  static constexpr int X_BYTES = OUT == Out::whole ? 2 * 2 * BM * 4 : 0;  // maxima and sums of the halves of a row
+  // biases of the fold warps' classes; maxima and sums of the halves of a row
+  static constexpr int X_BYTES = (OUT != Out::transposed ? kFoldWarps * HALF * 4 : 0) + (OUT == Out::whole ? 2 * 2 * BM * 4 : 0);
   static constexpr int BAR_OFF = X_OFF + X_BYTES;
   // more than half of an SM's shared memory: a second CTA, which would wait for tensor memory, never shares the SM
   static constexpr int NEED = BAR_OFF + 512 + 1024;
   static constexpr int SMEM_BYTES = NEED > 118 * 1024 ? NEED : 118 * 1024;
-  static_assert(NA % kConvGroups == 0 && NB % kConvGroups == 0 && NSB % kConvGroups == 0, "a slot belongs to one group");
-  // stages of A are not: a group that waits for stage g % NSA has seen the MMAs of k-block g - NSB retire
-  static_assert(NSB <= 2 * NSA, "the phase before the last of a stage of A has ended");
+  static_assert(NA % kSplitGroups == 0 && NB % kSplitGroups == 0, "a slot belongs to one group");
+  // Stages of terms are not: a group's wait for the MMAs of k-block g - NS is told from the phase before the last, k-block
+  // g - 2 NS, by the group's own last wait, for k-block g - kSplitGroups - NS.
+  static_assert(NSA >= kSplitGroups && NSB >= kSplitGroups, "the phase before the last of a stage has ended");
   static_assert(A_COL0 + NSA * A_COLS <= TMEM_COLS, "tensor memory has 512 columns");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
 };
@@ -263,8 +297,9 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
   uint64_t* free_a = full_a + (NA ? NA : 1);                           // slot read
   uint64_t* full_b = free_a + (NA ? NA : 1);
   uint64_t* free_b = full_b + NB;
-  uint64_t* ready = free_b + NB;          // [NSB] terms of a k-block in place (four warps)
-  uint64_t* empty_a = ready + NSB;        // [NSA] MMAs of the stage retired
+  uint64_t* ready_a = free_b + NB;        // [NSA] terms in place
+  uint64_t* ready_b = ready_a + NSA;      // [NSB]
+  uint64_t* empty_a = ready_b + NSB;      // [NSA] MMAs of the stage retired
   uint64_t* empty_b = empty_a + NSA;      // [NSB]
   uint64_t* acc_full = empty_b + NSB;     // [2]
   uint64_t* acc_empty = acc_full + 2;     // [2] read back by the fold warps
@@ -292,10 +327,13 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       mbar_init(&free_b[i], 4);
     }
     for (int i = 0; i < NSB; ++i) {
-      mbar_init(&ready[i], 4);
+      mbar_init(&ready_b[i], 4);
       mbar_init(&empty_b[i], 1);
     }
-    for (int i = 0; i < NSA; ++i) mbar_init(&empty_a[i], 1);
+    for (int i = 0; i < NSA; ++i) {
+      mbar_init(&ready_a[i], 4);
+      mbar_init(&empty_a[i], 1);
+    }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
       mbar_init(&acc_empty[i], kFoldWarps);
@@ -320,7 +358,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
   int w0, w_end, w_step;
   term_items<S>(args.total, w0, w_end, w_step);
 
-  if (warp < kConvWarp0) {
+  if (warp < kAWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if ((warp == 0 && A_TMA) || warp == 2) {
       // ---------------- TMA producers: warp 0 streams A, warp 2 streams B ----------------
@@ -336,7 +374,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
           const Product& p = args.p[wk.prob];
           for (int it = 0; it < wk.n_kb; ++it, ++g) {
             const uint32_t s = g % ring, ph = (g / ring) & 1;
-            ok = mbar_wait(&freed[s], ph ^ 1, is_a ? 41 : 42);
+            ok = mbar_wait_long(&freed[s], ph ^ 1, is_a ? 41 : 42);
             if (!ok) break;
             const int kx = (wk.kb0 + it) * BK;
             if (is_a) {
@@ -380,11 +418,11 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       for (int w = w0; ok && w < w_end; w += w_step) {
         const TermWork wk = term_work(args, w, BN);
         for (int it = 0; it < wk.n_kb; ++it, ++g) {
-          const uint32_t sa = g % NSA, sb = g % NSB, pb = (g / NSB) & 1;
+          const uint32_t sa = g % NSA, pa = (g / NSA) & 1, sb = g % NSB, pb = (g / NSB) & 1;
           const int in_fold = it % S::FOLD, in_small = it % (S::FOLD * kSmallFolds);
           if (in_fold == 0) ok = mbar_wait(&acc_empty[folds & 1], ((folds >> 1) & 1) ^ 1, 46);
           if (S::SMALL && ok && in_small == 0) ok = mbar_wait(small_empty, (smalls & 1) ^ 1, 47);
-          ok = ok && mbar_wait(&ready[sb], pb, 43);
+          ok = ok && mbar_wait(&ready_b[sb], pb, 43) && mbar_wait(&ready_a[sa], pa, 52);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -425,10 +463,10 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         }
       }
     }
-  } else if (warp < kFoldWarp0) {
-    // ---------------- terms of the operands (warps 4..15): every third k-block to a group ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
-    const int q = warp & 3, group = (warp - kConvWarp0) >> 2, row = 32 * q + lane;  // row of the A tile
+  } else if (warp < kBWarp0) {
+    // ---------------- terms of A (warps 4..11): every other k-block to a group ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsA));
+    const int q = warp & 3, group = (warp - kAWarp0) >> 2, row = 32 * q + lane;  // row of the tile
     uint32_t g = 0;
     bool ok = true;
     for (int w = w0; ok && w < w_end; w += w_step) {
@@ -436,48 +474,18 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       const Product& p = args.p[wk.prob];
       float a_sum = 0.f;
       const bool sums = p.a_sums != nullptr && wk.n0 == 0;
-      // steps of a packed B: a lane has the one of line q * 8 + lane / (BN / 32) of the k-block, block lane % (BN / 32) of the
-      // tile; fetched one k-block (of this group) ahead
-      uint32_t e_next = 0;
-      auto fetch_e = [&](int it) {
-        if constexpr (S::P8) {
-          constexpr int EB = BN / 32;
-          const int64_t k = (int64_t)(wk.kb0 + it) * BK + q * 8 + lane / EB;
-          const int b = wk.n0 / 32 + lane % EB;
-          e_next = it < wk.n_kb && lane < 8 * EB && k < p.k_rows && b < p.e_blocks ? p.e[k * p.lde + b] : 0u;
-        }
-      };
-      int it = (int)((group + kConvGroups - g % kConvGroups) % kConvGroups);  // first k-block of this group in the item
+      int it = (int)((g + group) % kSplitGroups);  // first k-block of this group in the item
       g += it;
-      fetch_e(it);
-      for (; it < wk.n_kb; it += kConvGroups, g += kConvGroups) {
-        const uint32_t sb = g % NSB, sa = g % NSA;
-        // ---- B ----
-        const uint32_t e8 = e_next;
-        fetch_e(it + kConvGroups);
+      for (; it < wk.n_kb; it += kSplitGroups, g += kSplitGroups) {
         float x[32];
-        if constexpr (!A_TMA) {  // on the way while B is split
+        if constexpr (!A_TMA) {
           const int64_t k0 = (int64_t)(wk.kb0 + it) * BK;
           const float* src = p.a + k0 * p.lda + wk.m0 + row;
           const bool col = wk.m0 + row < p.M;
 #pragma unroll
           for (int k = 0; k < 32; ++k) x[k] = col && k0 + k < p.k_rows ? __ldg(src + k * p.lda) : 0.f;
-        }
-        ok = __all_sync(0xffffffffu, mbar_wait(&full_b[g % NB], (g / NB) & 1, 44));  // the warp gives up as a whole
-        if (!ok) break;
-        TermB<S> tb;
-        tb.load(smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane);
-        ok = __all_sync(0xffffffffu, mbar_wait(&empty_b[sb], ((g / NSB) & 1) ^ 1, 45));
-        if (!ok) break;
-        tb.store(smem + S::T_OFF + sb * NTB * S::B_TERM, q, lane, e8);
-        __syncwarp();
-        // A slot is given back when what was made of it has been stored, not when it has been loaded: nothing keeps the loads
-        // themselves in front of the arrival (with it straight behind them results changed from run to run).
-        if (lane == 0) mbar_arrive(&free_b[g % NB]);
-        // ---- A ----
-        uint32_t t0[16], t1[16], t2[16];
-        if constexpr (A_TMA) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&full_a[g % NA], (g / NA) & 1, 48));
+        } else {
+          ok = __all_sync(0xffffffffu, mbar_wait_long(&full_a[g % NA], (g / NA) & 1, 48));  // the warp gives up as a whole
           if (!ok) break;
           const uint8_t* slot = smem + (g % NA) * A_SLOT;
           if constexpr (S::A == ASrc::kMajor) {
@@ -500,9 +508,11 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
           for (int k = 0; k < 8; ++k) s8[k] = (x[k] + x[k + 8]) + (x[k + 16] + x[k + 24]);
           a_sum += ((s8[0] + s8[1]) + (s8[2] + s8[3])) + ((s8[4] + s8[5]) + (s8[6] + s8[7]));
         }
+        uint32_t t0[16], t1[16], t2[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) split3(x[2 * k], x[2 * k + 1], t0[k], t1[k], t2[k]);
-        ok = __all_sync(0xffffffffu, mbar_wait(&empty_a[sa], ((g / NSA) & 1) ^ 1, 49));
+        const uint32_t sa = g % NSA;
+        ok = __all_sync(0xffffffffu, mbar_wait_long(&empty_a[sa], ((g / NSA) & 1) ^ 1, 49));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t ta = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(S::A_COL0 + sa * S::A_COLS);
@@ -511,20 +521,64 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         tmem_st16(ta + 32, t2);
         if constexpr (A_TMA) {
           __syncwarp();
+          // A slot is given back when what was made of it has been stored, not when it has been loaded: nothing keeps the
+          // loads themselves in front of the arrival (with it straight behind them results changed from run to run).
           if (lane == 0) mbar_arrive(&free_a[g % NA]);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the MMA
         __syncwarp();
-        if (lane == 0) mbar_arrive(&ready[sb]);
+        if (lane == 0) mbar_arrive(&ready_a[sa]);
       }
       if (!ok) break;
       g -= it - wk.n_kb;  // k-blocks of all groups
-      if (sums && wk.m0 + row < p.M) p.a_sums[(kConvGroups * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
+      if (sums && wk.m0 + row < p.M) p.a_sums[(kSplitGroups * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
+    }
+  } else if (warp < kFoldWarp0) {
+    // ---------------- terms of B (warps 12..19) ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsB));
+    const int q = warp & 3, group = (warp - kBWarp0) >> 2;
+    uint32_t g = 0;
+    bool ok = true;
+    for (int w = w0; ok && w < w_end; w += w_step) {
+      const TermWork wk = term_work(args, w, BN);
+      const Product& p = args.p[wk.prob];
+      // steps of a packed B: a lane has the one of line q * 8 + lane / (BN / 32) of the k-block, block lane % (BN / 32) of the
+      // tile; fetched one k-block (of this group) ahead
+      uint32_t e_next = 0;
+      auto fetch_e = [&](int it) {
+        if constexpr (S::P8) {
+          constexpr int EB = BN / 32;
+          const int64_t k = (int64_t)(wk.kb0 + it) * BK + q * 8 + lane / EB;
+          const int b = wk.n0 / 32 + lane % EB;
+          e_next = it < wk.n_kb && lane < 8 * EB && k < p.k_rows && b < p.e_blocks ? p.e[k * p.lde + b] : 0u;
+        }
+      };
+      int it = (int)((g + group) % kSplitGroups);
+      g += it;
+      fetch_e(it);
+      for (; it < wk.n_kb; it += kSplitGroups, g += kSplitGroups) {
+        const uint32_t sb = g % NSB, e8 = e_next;
+        fetch_e(it + kSplitGroups);
+        ok = __all_sync(0xffffffffu, mbar_wait_long(&full_b[g % NB], (g / NB) & 1, 44));
+        if (!ok) break;
+        TermB<S> tb;
+        tb.load(smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane);
+        ok = __all_sync(0xffffffffu, mbar_wait_long(&empty_b[sb], ((g / NSB) & 1) ^ 1, 45));
+        if (!ok) break;
+        tb.store(smem + S::T_OFF + sb * NTB * S::B_TERM, q, lane, e8);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the MMA
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&free_b[g % NB]);
+          mbar_arrive(&ready_b[sb]);
+        }
+      }
+      if (!ok) break;
+      g -= it - wk.n_kb;
     }
   } else {
-    // ---------------- folds and results (warps 16..23) ----------------
+    // ---------------- folds and results (warps 20..27) ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsFold));
     const int quad = warp & 3, half = (warp - kFoldWarp0) >> 2;
     const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + half * HALF;
@@ -558,7 +612,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
 #pragma unroll
       for (int j = 0; j < HALF; ++j) sum[j] = 0.f;
       for (int it = 0; it < wk.n_kb; it += S::FOLD, ++folds) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[folds & 1], (folds >> 1) & 1, 50));
+        ok = __all_sync(0xffffffffu, mbar_wait_long(&acc_full[folds & 1], (folds >> 1) & 1, 50));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int done = it + S::FOLD;
@@ -600,35 +654,54 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         const int cols = min(HALF, p.N - nb);  // classes of this half (may be below 1)
         const int c0 = args.ce.c0 + nb;
         if (args.ce.bias) {
+          float* const xb = reinterpret_cast<float*>(smem + S::X_OFF) + (warp - kFoldWarp0) * HALF;
+#pragma unroll
+          for (int j = 0; j < HALF; j += 32) xb[j + lane] = j + lane < cols ? __ldg(args.ce.bias + c0 + j + lane) : 0.f;
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < HALF; j += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(xb + j);
+            sum[j] += b.x; sum[j + 1] += b.y; sum[j + 2] += b.z; sum[j + 3] += b.w;
+          }
+          __syncwarp();
+        }
+        if (cols < HALF) {
 #pragma unroll
           for (int j = 0; j < HALF; ++j)
-            if (j < cols) sum[j] += __ldg(args.ce.bias + c0 + j);
+            if (j >= cols) sum[j] = -INFINITY;
         }
         label -= c0;  // relative to this half
+        const bool here = row_in && label >= 0 && label < cols;
+        const bool any_here = __any_sync(0xffffffffu, here);  // (few of the tiles have a label of a warp's rows)
         if constexpr (S::OUT == Out::grad) {
-          float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
-          if (row_in)
+          const float scale = args.ce.inv_nt, shift = -lse;
+#pragma unroll
+          for (int j = 0; j < HALF; ++j) sum[j] = exp2_fast((sum[j] + shift) * kLog2e);
+          if (any_here)
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) sum[j] -= j == label ? 1.f : 0.f;
+          if (row_in) {
+            float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
+            const int64_t ldg = args.ce.ldg;
 #pragma unroll
             for (int j = 0; j < HALF; ++j)
-              if (j < cols) gt[(int64_t)j * args.ce.ldg] = (expf(sum[j] - lse) - (j == label ? 1.f : 0.f)) * args.ce.inv_nt;
+              if (j < cols) gt[j * ldg] = sum[j] * scale;
+          }
         } else {
           float mx = -INFINITY, zy = 0.f;
 #pragma unroll
-          for (int j = 0; j < HALF; ++j)
-            if (j < cols) {
-              mx = fmaxf(mx, sum[j]);
-              if (j == label) zy = sum[j];
-            }
-          const bool here = label >= 0 && label < cols;
+          for (int j = 0; j < HALF; ++j) mx = fmaxf(mx, sum[j]);
+          if (any_here)
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) zy = j == label ? sum[j] : zy;
           if constexpr (S::OUT == Out::stats) {
-            if (here && row_in) args.ce.zy[m] = zy;
+            if (here) args.ce.zy[m] = zy;
             // the run's maximum and sum go on; a maximum of -infinity has nothing to be subtracted from
             const float top = fmaxf(run_m, mx), base = top == -INFINITY ? 0.f : top;
-            float s = 0.f;
+            float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < HALF; ++j)
-              if (j < cols) s += expf(sum[j] - base);
-            run_s = run_s * expf(run_m - base) + s;
+            for (int j = 0; j < HALF; ++j) s4[j & 3] += exp2_fast((sum[j] - base) * kLog2e);
+            run_s = run_s * exp2_fast((run_m - base) * kLog2e) + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
             run_m = top;
             const int next = w + 1;
             if (next >= w_end || next / p.tiles_n != w / p.tiles_n) {
@@ -640,19 +713,20 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
             }
           } else {
             // both halves of a row: maxima, then sums and the label's logit, through shared memory
-            float* xm = reinterpret_cast<float*>(smem + S::X_OFF);
+            float* xm = reinterpret_cast<float*>(smem + S::X_OFF) + kFoldWarps * HALF;
             float* xs = xm + 2 * BM;
             const int r = quad * 32 + lane;
             xm[half * BM + r] = mx;
             ok = meet();
             if (!ok) break;
             const float top = fmaxf(xm[r], xm[BM + r]), base = top == -INFINITY ? 0.f : top;
-            float s = 0.f;
+            float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < HALF; ++j) {
-              sum[j] = j < cols ? expf(sum[j] - base) : 0.f;
-              s += sum[j];
+              sum[j] = exp2_fast((sum[j] - base) * kLog2e);
+              s4[j & 3] += sum[j];
             }
+            float s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
             xs[half * BM + r] = s;
             ok = meet();
             if (!ok) break;
@@ -663,9 +737,10 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
                 args.ce.row_loss[m] = !on ? 0.f : here ? (base + logf(s)) - zy : NAN;
               if (args.ce.gt) {
                 float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
+                const int64_t ldg = args.ce.ldg;
 #pragma unroll
                 for (int j = 0; j < HALF; ++j)
-                  if (j < cols) gt[(int64_t)j * args.ce.ldg] = on ? (sum[j] * inv - (j == label ? 1.f : 0.f)) * args.ce.inv_nt : 0.f;
+                  if (j < cols) gt[j * ldg] = on ? (sum[j] * inv - (j == label ? 1.f : 0.f)) * args.ce.inv_nt : 0.f;
               }
             }
           }
