@@ -29,17 +29,36 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Slices of the inner dimension: as many as make the rounds of tiles x slices items over the SMs shortest, a slice costing
 // about six k-blocks on top of its own (its share of the sums written and read again, an accumulator's start and end).
-int pick_slices(int64_t tiles, int64_t units) {
-  const int64_t sms = sm_count();
-  int64_t best = 1, best_cost = INT64_MAX;
-  for (int64_t s = 1; s <= std::min<int64_t>(units, std::max<int64_t>(1, 2 * sms / tiles)); ++s) {
-    const int64_t cost = div_up(tiles * s, sms) * (div_up(units, s) + 6);
-    if (cost < best_cost) {
+template <class Cost>
+int cheapest_slices(int64_t tiles, int64_t units, Cost cost) {
+  const int most = (int)std::min<int64_t>(units, std::max<int64_t>(1, 2 * sm_count() / tiles));
+  int best = 1, best_cost = INT32_MAX;
+  for (int s = 1; s <= most; s += std::max(1, s / 16)) {  // (one in 16 apart: the search runs in every call)
+    const int len = (int)div_up(units, s), c = cost((int)div_up(units, len), len);
+    if (c < best_cost) {
       best = s;
-      best_cost = cost;
+      best_cost = c;
     }
   }
   return (int)div_up(units, div_up(units, best));
+}
+int pick_slices(int64_t tiles, int64_t units) {
+  const int sms = sm_count(), t = (int)tiles;
+  return cheapest_slices(tiles, units, [&](int s, int len) { return (t * s + sms - 1) / sms * (len + 6); });
+}
+// The same for a product whose items are followed in a launch by `others` items of other_units k-blocks.  Block b takes items b,
+// b + grid, ...: what the fullest block gets, which is the first one or the first with an item less of either kind.
+int balanced_slices(int64_t tiles, int64_t units, int64_t others, int64_t other_units) {
+  const int sms = sm_count(), t = (int)tiles, o = (int)others;
+  return cheapest_slices(tiles, units, [&](int s, int len) {
+    const int items = t * s, total = items + o, grid = std::min(total, sms);
+    int most = 0;
+    for (const int b : {0, items % grid, total % grid}) {
+      const int mine = items > b ? (items - b + grid - 1) / grid : 0, all = (total - b + grid - 1) / grid;
+      most = std::max(most, mine * (len + 6) + (all - mine) * ((int)other_units + 6));
+    }
+    return most;
+  });
 }
 void set_slices(Product& p, int bn, int slices) {
   p.tiles_m = (int)div_up(p.M, BM);
@@ -205,16 +224,49 @@ loss_total(int blocks, const LossSum* __restrict__ partial, const int* __restric
   }
   finish_loss(a, total ? *total : a.count, n_train, loss);
 }
-// out[j] (+)= sum over `lines` lines of sums[i * pitch + j]
+// The slices of a product added up, and with them the sums that its left operand left: row r of c (+)= sum over the slices of
+// partial[z][r][.] for r < rows, and sums_out (+)= sum over `lines` lines of sums.  A block has 128 columns of a row; its 8 warps
+// take every 8th slice each, a float4 to a lane, and are added in warp order.
 __global__ void __launch_bounds__(256)
-sum_lines(int n, int lines, const float* __restrict__ sums, int64_t pitch, float* __restrict__ out, int accumulate) {
+add_slices(int rows, int n, int slices, const float* __restrict__ partial, int64_t ldp, float* __restrict__ c, int64_t ldc, int n_pad, int lines,
+           const float* __restrict__ sums, float* __restrict__ sums_out, int accumulate) {
   wait_for_predecessors();
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= n) return;
-  float s = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < lines; ++i) s += sums[i * pitch + j];
-  out[j] = accumulate ? out[j] + s : s;
+  __shared__ float4 sh[8][32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, j = 128 * blockIdx.x + 4 * lane;
+  for (int r = blockIdx.y; r < rows + (sums_out != nullptr); r += gridDim.y) {
+    const bool tail = r == rows;
+    const float* src = tail ? sums + j : partial + r * ldp + j;
+    const int64_t step = tail ? ldp : rows * ldp;
+    const int count = tail ? lines : slices;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (j < n) {
+#pragma unroll 4
+      for (int z = w; z < count; z += 8) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(src + z * step));
+        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+      }
+    }
+    sh[w][lane] = a;
+    __syncthreads();
+    if (threadIdx.x < 128) {
+      const int k = threadIdx.x, col = 128 * blockIdx.x + k;
+      float s = 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s += reinterpret_cast<const float*>(sh[q])[k];
+      float* const dst = tail ? sums_out + col : c + r * ldc + col;
+      if (col < n) *dst = accumulate ? *dst + s : s;
+      else if (!tail && col < n_pad && !accumulate) *dst = 0.f;
+    }
+    __syncthreads();
+  }
+}
+// (pitch of both partial and sums: ldp)
+int launch_add_slices(cudaStream_t s, int64_t rows, int64_t n, int slices, const float* partial, int64_t ldp, float* c, int64_t ldc, int64_t n_pad,
+                      int lines, const float* sums, float* sums_out, int accumulate) {
+  const dim3 grid((unsigned)((n_pad + 127) / 128), (unsigned)std::min<int64_t>(rows + (sums_out != nullptr), 65535));
+  const cudaError_t e = launch(add_slices, grid, 256, 0, s, rows, n, slices, partial, ldp, c, ldc, n_pad, lines, sums, sums_out, accumulate);
+  note_launch();
+  return (int)e;
 }
 
 // ---- plan of a call: sizes that hold for every count of rows up to n -------------------------------------------------
@@ -284,7 +336,7 @@ size_t gemm_packed8_workspace(int64_t n, int32_t f, int32_t c) {
 
 int launch_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g, int64_t ldg,
                         float* dw, int64_t lddw, int32_t accumulate, void* workspace) {
-  if (n <= 0) return launch_splitk_reduce(stream, f, c, 0, nullptr, up4(c), dw, lddw, accumulate, GCNSA_EPI_NONE, nullptr, 0);
+  if (n <= 0) return launch_add_slices((cudaStream_t)stream, f, c, 0, nullptr, up4(c), dw, lddw, std::min<int64_t>(lddw, up4(c)), 0, nullptr, nullptr, accumulate);
   const PackedPlan pl = packed_plan(n, f, c);
   const bool tma = ((uintptr_t)g & 15) == 0 && ldg % 4 == 0;
   TermArgs a = {};
@@ -314,7 +366,7 @@ int launch_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcn
   GCNSA_STEP(pl.bn == 64 ? (tma ? run_packed<64, ASrc::mnMajor>(s, a, grid) : run_packed<64, ASrc::direct>(s, a, grid))
                          : (tma ? run_packed<128, ASrc::mnMajor>(s, a, grid) : run_packed<128, ASrc::direct>(s, a, grid)));
   note_launch();
-  if (split) return launch_splitk_reduce(stream, f, c, pl.slices, (const float*)workspace, pl.ldp, dw, lddw, accumulate, GCNSA_EPI_NONE, nullptr, 0);
+  if (split) return launch_add_slices(s, f, c, pl.slices, (const float*)workspace, pl.ldp, dw, lddw, std::min<int64_t>(lddw, up4(c)), 0, nullptr, nullptr, accumulate);
   return 0;
 }
 
@@ -408,11 +460,8 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
   }
   if (!grads) return 0;
   if (R == 0) {  // nothing counts: sums of nothing
-    if (a.dw) GCNSA_STEP(launch_splitk_reduce(stream, a.d, a.c, 0, nullptr, up4(a.c), a.dw, a.lddw, a.accumulate, GCNSA_EPI_NONE, nullptr, 0));
-    if (a.db) {
-      GCNSA_STEP(launch(sum_lines, (int)div_up(a.c, 256), 256, 0, s, a.c, 0, (const float*)nullptr, (int64_t)0, a.db, a.accumulate));
-      note_launch();
-    }
+    if (a.dw || a.db)
+      GCNSA_STEP(launch_add_slices(s, a.dw ? a.d : 0, a.c, 0, nullptr, up4(a.c), a.dw, a.lddw, a.dw ? std::min<int64_t>(a.lddw, up4(a.c)) : a.c, 0, nullptr, a.db, a.accumulate));
     return 0;
   }
   const int64_t piece = whole ? a.c : piece_classes(pl, R, a.c);
@@ -431,6 +480,8 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     TermArgs b = {};
     Product &pw = b.p[0], &ph = b.p[1];
     const bool weights = a.dw || a.db;
+    // pad columns belong to the last piece
+    const int64_t dw_pad = a.dw && c0 + width == a.c ? std::min<int64_t>(a.lddw - c0, up4(width)) : width;
     int slices = 1;
     if (weights) {
       if (!term_map(&pw.map_a, f_at(pl.gt), false, width, R, ldg, BK, BM, true) || !term_map(&pw.map_b, h, false, R, a.d, ldh, 32, BK, false))
@@ -438,7 +489,8 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
       pw.M = (int)width;
       pw.N = a.d;
       pw.units = (int)div_up(R, BK);
-      slices = pick_slices(div_up(width, BM) * div_up(a.d, 128), pw.units);
+      // (also where dh is not asked for: the same slices, the same bits)
+      slices = balanced_slices(div_up(width, BM) * div_up(a.d, 128), pw.units, div_up(a.d, BM) * div_up(R, 128), div_up(width, BK));
       set_slices(pw, 128, slices);
       const bool split = slices > 1;
       pw.write = a.dw != nullptr;
@@ -446,8 +498,7 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
       pw.ldc = split ? up4(width) : a.lddw;
       pw.slice_stride = split ? a.d * up4(width) : 0;
       pw.accumulate = split ? 0 : a.accumulate;
-      // pad columns belong to the last piece
-      pw.m_pad = (int)(split ? up4(width) : c0 + width < a.c ? width : std::min<int64_t>(a.lddw - c0, up4(width)));
+      pw.m_pad = (int)(split ? up4(width) : dw_pad);
       pw.k_rows = R;
       if (a.db) {
         pw.a_sums = f_at(pl.sums);
@@ -472,12 +523,10 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     b.total = pw.items + ph.items;
     GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::transposed>>(s, b, std::min(b.total, sms))));
     note_launch();
-    if (a.dw && slices > 1)
-      GCNSA_STEP(launch_splitk_reduce(stream, a.d, width, slices, (const float*)f_at(pl.partial), up4(width), a.dw + c0, a.lddw, a.accumulate, GCNSA_EPI_NONE, nullptr, 0));
-    if (a.db) {
-      GCNSA_STEP(launch(sum_lines, (int)div_up(width, 256), 256, 0, s, (int)width, kSplitGroups * slices, (const float*)f_at(pl.sums), up4(width), a.db + c0, a.accumulate));
-      note_launch();
-    }
+    const bool add = a.dw && slices > 1;
+    if (add || a.db)
+      GCNSA_STEP(launch_add_slices(s, add ? a.d : 0, width, slices, f_at(pl.partial), up4(width), add ? a.dw + c0 : nullptr, a.lddw, add ? dw_pad : width,
+                                   kSplitGroups * slices, f_at(pl.sums), a.db ? a.db + c0 : nullptr, a.accumulate));
   }
   return 0;
 }

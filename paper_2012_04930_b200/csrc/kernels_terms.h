@@ -474,16 +474,19 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       const Product& p = args.p[wk.prob];
       float a_sum = 0.f;
       const bool sums = p.a_sums != nullptr && wk.n0 == 0;
+      // (fields of p are copied where a loop uses them: with the product's index a variable each would be a load every time)
+      const float* const a_at = A_TMA ? nullptr : p.a + wk.m0 + row;
+      const int64_t lda = p.lda, k_rows = p.k_rows;
+      const bool in_m = wk.m0 + row < p.M;
       int it = (int)((g + group) % kSplitGroups);  // first k-block of this group in the item
       g += it;
       for (; it < wk.n_kb; it += kSplitGroups, g += kSplitGroups) {
         float x[32];
         if constexpr (!A_TMA) {
           const int64_t k0 = (int64_t)(wk.kb0 + it) * BK;
-          const float* src = p.a + k0 * p.lda + wk.m0 + row;
-          const bool col = wk.m0 + row < p.M;
+          const float* src = a_at + k0 * lda;
 #pragma unroll
-          for (int k = 0; k < 32; ++k) x[k] = col && k0 + k < p.k_rows ? __ldg(src + k * p.lda) : 0.f;
+          for (int k = 0; k < 32; ++k) x[k] = in_m && k0 + k < k_rows ? __ldg(src + k * lda) : 0.f;
         } else {
           ok = __all_sync(0xffffffffu, mbar_wait_long(&full_a[g % NA], (g / NA) & 1, 48));  // the warp gives up as a whole
           if (!ok) break;
@@ -532,7 +535,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       }
       if (!ok) break;
       g -= it - wk.n_kb;  // k-blocks of all groups
-      if (sums && wk.m0 + row < p.M) p.a_sums[(kSplitGroups * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
+      if (sums && in_m) p.a_sums[(kSplitGroups * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
     }
   } else if (warp < kFoldWarp0) {
     // ---------------- terms of B (warps 12..19) ----------------
@@ -546,13 +549,12 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       // steps of a packed B: a lane has the one of line q * 8 + lane / (BN / 32) of the k-block, block lane % (BN / 32) of the
       // tile; fetched one k-block (of this group) ahead
       uint32_t e_next = 0;
+      constexpr int EB = BN / 32;
+      const int64_t lde = p.lde, k_left = p.k_rows - ((int64_t)wk.kb0 * BK + q * 8 + lane / EB);
+      const uint8_t* const e_at = p.e + (p.k_rows - k_left) * lde + wk.n0 / 32 + lane % EB;
+      const bool e_in = S::P8 && lane < 8 * EB && wk.n0 / 32 + lane % EB < p.e_blocks;
       auto fetch_e = [&](int it) {
-        if constexpr (S::P8) {
-          constexpr int EB = BN / 32;
-          const int64_t k = (int64_t)(wk.kb0 + it) * BK + q * 8 + lane / EB;
-          const int b = wk.n0 / 32 + lane % EB;
-          e_next = it < wk.n_kb && lane < 8 * EB && k < p.k_rows && b < p.e_blocks ? p.e[k * p.lde + b] : 0u;
-        }
+        if constexpr (S::P8) e_next = e_in && it < wk.n_kb && it * BK < k_left ? __ldg(e_at + (int64_t)it * BK * lde) : 0u;
       };
       int it = (int)((g + group) % kSplitGroups);
       g += it;
@@ -640,14 +642,36 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       if (!ok) break;
       if constexpr (S::OUT == Out::transposed) {
         if (p.write && m < p.m_pad) {
-          float* dst = p.c + wk.z * p.slice_stride + m;
+          // (with what is there added) 8 lines at a time: where they go, what is there, then the stores (one by one every load would wait for the store
+          // before it, as the compiler cannot tell that the lines differ)
+          float* const dst = p.c + wk.z * p.slice_stride + m;
+          const int32_t* const row_map = p.row_map;
+          const int64_t ldc = p.ldc;
+          const int left = p.N - nb;
+          const bool add = p.accumulate != 0;
+          if (!row_map && !add) {
+            float* at = dst + nb * ldc;
 #pragma unroll
-          for (int j = 0; j < HALF; ++j) {
-            if (nb + j >= p.N) break;
-            const int64_t r = p.row_map ? __ldg(p.row_map + nb + j) : nb + j;
-            if (r < 0) continue;
-            float* at = dst + r * p.ldc;
-            *at = p.accumulate ? *at + sum[j] : sum[j];
+            for (int j = 0; j < HALF; ++j, at += ldc)
+              if (j < left) *at = sum[j];
+          } else {
+#pragma unroll
+            for (int j0 = 0; j0 < HALF; j0 += 8) {
+              if (j0 >= left) break;
+              int r[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) r[j] = j0 + j >= left ? -1 : row_map ? __ldg(row_map + nb + j0 + j) : nb + j0 + j;
+              if (add) {
+                float was[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) was[j] = r[j] >= 0 ? dst[r[j] * ldc] : 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j0 + j] += was[j];
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (r[j] >= 0) dst[r[j] * ldc] = sum[j0 + j];
+            }
           }
         }
       } else {

@@ -752,41 +752,62 @@ def _refuse(what):
     raise GcnsaError(ERR_ARG, what)
 
 
-def _operand(t, name, dtype, rows=None, cols=None, like=None):
-    """(pointer, leading dimension) of a device tensor: [rows x >= cols] with contiguous columns, or (cols None) a contiguous
-    vector of at least `rows` elements."""
+_torch_api = None
+
+
+def _torch():
+    """(torch, its dtypes by name, raw stream of a device, current device): looked up once, as these calls cost more host time
+    than the launches of a small operator."""
+    global _torch_api
+    if _torch_api is None:
+        import torch
+        dtypes = {n: getattr(torch, n) for n in ("float32", "int32", "int8", "uint8")}
+        _torch_api = (torch, dtypes, torch._C._cuda_getCurrentRawStream, torch.cuda.current_device)
+    return _torch_api
+
+
+def _vector(t, name, dtype, size, dev):
+    """Pointer of a contiguous device vector of at least `size` elements, or None."""
+    if t is None:
+        return None
+    if t.get_device() != dev or t.dtype is not _torch()[1][dtype] or not t.is_contiguous() or t.numel() < size:
+        _refuse(f"{name}: a contiguous {dtype} vector of {size} elements on cuda:{dev} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _matrix(t, name, dtype, rows, cols, dev):
+    """(pointer, leading dimension) of a device matrix [rows x at least cols] whose columns are contiguous, or (None, 0)."""
     if t is None:
         return None, 0
-    if not t.is_cuda or (like is not None and t.device != like.device):
-        _refuse(f"{name}: on {t.device}, expected {'a CUDA device' if like is None else like.device}")
-    if str(t.dtype) != "torch." + dtype:
-        _refuse(f"{name}: {t.dtype}, expected {dtype}")
-    if cols is None:
-        if t.numel() < (rows or 0) or not t.is_contiguous():
-            _refuse(f"{name}: a contiguous vector of {rows} elements is needed, got {tuple(t.shape)}")
-        return _dp(t), 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1):
-        _refuse(f"{name}: rows of contiguous columns are needed, [{rows} x at least {cols}], got {tuple(t.shape)} with strides {t.stride()}")
+    shape = t.shape
+    if (len(shape) != 2 or shape[0] != rows or shape[1] < cols or t.get_device() != dev or t.dtype is not _torch()[1][dtype] or
+            (shape[1] > 1 and t.stride(1) != 1)):
+        _refuse(f"{name}: rows of contiguous {dtype} columns on cuda:{dev} are needed, [{rows} x at least {cols}], got {t.dtype} "
+                f"{tuple(shape)} with strides {t.stride() if t.dim() else ()} on {t.device}")
     # (the stride of a single row says nothing)
-    return _dp(t), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], cols)
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(shape[1], cols)
 
 
-def _on(t):
-    """The stream that a call on t's device goes to; that device has to be the current one."""
-    import torch
-    if t.device.index != torch.cuda.current_device():
-        _refuse(f"tensors on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream()
+def _bytes_of(t, name, dev):
+    """(pointer, size) of scratch memory of any type."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(f"{name}: contiguous memory on cuda:{dev} is needed, got {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _nbytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
-
-
-def _rows_of(t, name):
+def _leader(t, name):
+    """(rows, device index, stream) of the matrix whose device the call goes to; that device has to be the current one."""
     if t is None or t.dim() != 2:
         _refuse(f"{name}: a matrix is needed")
-    return t.shape[0]
+    dev = t.get_device()
+    if dev < 0:
+        _refuse(f"{name}: on {t.device}, a CUDA device is needed")
+    _, _, raw_stream, current = _torch()
+    if dev != current():
+        _refuse(f"{name}: on cuda:{dev}, the current device is cuda:{current()}")
+    return t.shape[0], dev, raw_stream(dev)
 
 
 class Packed8:
@@ -802,46 +823,43 @@ class Packed8:
         self.q = torch.zeros((n, (f + 15) // 16 * 16), dtype=torch.int8, device=dev) if q is None else q
         self.e = torch.zeros((n, (f + 31) // 32), dtype=torch.uint8, device=dev) if e is None else e
 
-    def dev(self, name="checkpoint", n=None, f=None, like=None) -> Packed8Dev:
-        if (n is not None and n != self.n) or (f is not None and f != self.f):
+    def on(self, name, n, f, dev):
+        """What the library is handed."""
+        if n != self.n or f != self.f:
             _refuse(f"{name}: {self.n} x {self.f}, expected {n} x {f}")
-        q, ldq = _operand(self.q, name + ".q", "int8", self.n, (self.f + 15) // 16 * 16, like)
-        e, lde = _operand(self.e, name + ".e", "uint8", self.n, (self.f + 31) // 32, self.q)
-        return Packed8Dev(q=q, ldq=ldq, e=e, lde=lde)
-
-
-def _packed(p, name, n, f, like):
-    return None if p is None else C.byref(p.dev(name, n, f, like))
+        q, ldq = _matrix(self.q, name + ".q", "int8", self.n, (self.f + 15) // 16 * 16, dev)
+        e, lde = _matrix(self.e, name + ".e", "uint8", self.n, (self.f + 31) // 32, dev)
+        return C.byref(Packed8Dev(q, ldq, e, lde))
 
 
 def op_layer_norm(x, f, y, gamma=None, beta=None, eps=1e-5, relu=0, mean=None, rstd=None, x8=None, y8=None, bits=None):
     """y = norm of the rows of x (first f columns), then gamma, beta and (relu) ReLU; mean and rstd per row are what the
     backward pass needs; x8 and y8 (Packed8) receive checkpoints of x and of y, bits (int32 [n x ceil(f / 32)]) what the ReLU
     let through."""
-    n = _rows_of(x, "x")
-    xp, ldx = _operand(x, "x", "float32", n, f)
-    yp, ldy = _operand(y, "y", "float32", n, f, x)
-    vec = [_operand(t, nm, "float32", k, None, x)[0] for t, nm, k in ((gamma, "gamma", f), (beta, "beta", f), (mean, "mean", n), (rstd, "rstd", n))]
-    _ck(lib().gcnsa_op_layer_norm(_on(x), n, f, xp, ldx, vec[0], vec[1], eps, int(relu), yp, ldy, vec[2], vec[3],
-                                  _packed(x8, "x8", n, f, x), _packed(y8, "y8", n, f, x),
-                                  *_operand(bits, "bits", "int32", n, (f + 31) // 32, x)))
+    n, dev, stream = _leader(x, "x")
+    xp, ldx = _matrix(x, "x", "float32", n, f, dev)
+    yp, ldy = _matrix(y, "y", "float32", n, f, dev)
+    bp, ldb = _matrix(bits, "bits", "int32", n, (f + 31) // 32, dev)
+    _ck(lib().gcnsa_op_layer_norm(stream, n, f, xp, ldx, _vector(gamma, "gamma", "float32", f, dev), _vector(beta, "beta", "float32", f, dev),
+                                  eps, int(relu), yp, ldy, _vector(mean, "mean", "float32", n, dev), _vector(rstd, "rstd", "float32", n, dev),
+                                  None if x8 is None else x8.on("x8", n, f, dev), None if y8 is None else y8.on("y8", n, f, dev), bp, ldb))
 
 
 def op_layer_norm_backward(g, x, f, dx, mean, rstd, gamma=None, beta=None, relu=0, dgamma=None, dbeta=None, accumulate=0,
                            scratch=None, bits=None):
     """dx (and dgamma, dbeta) of op_layer_norm from the gradient g w.r.t. its result; x is its input or a Packed8 of it, bits
     what the forward pass said of the ReLU (without: taken from x)."""
-    n = _rows_of(g, "g")
-    gp, ldg = _operand(g, "g", "float32", n, f)
-    dxp, lddx = _operand(dx, "dx", "float32", n, f, g)
-    x8 = _packed(x, "x", n, f, g) if isinstance(x, Packed8) else None
-    xp, ldx = (None, 0) if x8 is not None else _operand(x, "x", "float32", n, f, g)
-    vec = [_operand(t, nm, "float32", k, None, g)[0] for t, nm, k in
-           ((mean, "mean", n), (rstd, "rstd", n), (gamma, "gamma", f), (beta, "beta", f), (dgamma, "dgamma", f), (dbeta, "dbeta", f))]
-    if scratch is not None:
-        _operand(scratch, "scratch", str(scratch.dtype)[6:], 0, None, g)
-    _ck(lib().gcnsa_op_layer_norm_backward(_on(g), n, f, gp, ldg, xp, ldx, x8, vec[0], vec[1], vec[2], vec[3], int(relu),
-                                           *_operand(bits, "bits", "int32", n, (f + 31) // 32, g), dxp, lddx, vec[4], vec[5], accumulate, _dp(scratch), _nbytes(scratch)))
+    n, dev, stream = _leader(g, "g")
+    gp, ldg = _matrix(g, "g", "float32", n, f, dev)
+    dxp, lddx = _matrix(dx, "dx", "float32", n, f, dev)
+    x8 = x.on("x", n, f, dev) if isinstance(x, Packed8) else None
+    xp, ldx = (None, 0) if x8 is not None else _matrix(x, "x", "float32", n, f, dev)
+    bp, ldb = _matrix(bits, "bits", "int32", n, (f + 31) // 32, dev)
+    _ck(lib().gcnsa_op_layer_norm_backward(
+        stream, n, f, gp, ldg, xp, ldx, x8, _vector(mean, "mean", "float32", n, dev), _vector(rstd, "rstd", "float32", n, dev),
+        _vector(gamma, "gamma", "float32", f, dev), _vector(beta, "beta", "float32", f, dev), int(relu), bp, ldb, dxp, lddx,
+        _vector(dgamma, "dgamma", "float32", f, dev), _vector(dbeta, "dbeta", "float32", f, dev), accumulate,
+        *_bytes_of(scratch, "scratch", dev)))
 
 
 def op_layer_norm_backward_scratch(n, f) -> int:
@@ -850,24 +868,25 @@ def op_layer_norm_backward_scratch(n, f) -> int:
 
 def op_pack8(x, p):
     """Checkpoint of the first p.f columns of x."""
-    xp, ldx = _operand(x, "x", "float32", p.n, p.f)
-    _ck(lib().gcnsa_op_pack8(_on(x), p.n, p.f, xp, ldx, _packed(p, "p", None, None, x)))
+    n, dev, stream = _leader(x, "x")
+    xp, ldx = _matrix(x, "x", "float32", n, p.f, dev)
+    _ck(lib().gcnsa_op_pack8(stream, n, p.f, xp, ldx, p.on("p", n, p.f, dev)))
 
 
 def op_unpack8(p, x):
     """x = what the checkpoint stands for (first p.f columns)."""
-    xp, ldx = _operand(x, "x", "float32", p.n, p.f)
-    _ck(lib().gcnsa_op_unpack8(_on(x), p.n, p.f, _packed(p, "p", None, None, x), xp, ldx))
+    n, dev, stream = _leader(x, "x")
+    xp, ldx = _matrix(x, "x", "float32", n, p.f, dev)
+    _ck(lib().gcnsa_op_unpack8(stream, n, p.f, p.on("p", n, p.f, dev), xp, ldx))
 
 
 def op_gemm_packed8(p, g, c, dw, accumulate=0, workspace=None):
     """dw (+)= X^T G with X a checkpoint [n x f] and G the first c columns of g."""
-    gp, ldg = _operand(g, "g", "float32", p.n, c)
-    dwp, lddw = _operand(dw, "dw", "float32", p.f, c, g)
-    if workspace is not None:
-        _operand(workspace, "workspace", str(workspace.dtype)[6:], 0, None, g)
-    _ck(lib().gcnsa_op_gemm_packed8(_on(g), p.n, p.f, c, _packed(p, "p", None, None, g), gp, ldg, dwp, lddw, accumulate,
-                                    _dp(workspace), _nbytes(workspace)))
+    n, dev, stream = _leader(g, "g")
+    gp, ldg = _matrix(g, "g", "float32", n, c, dev)
+    dwp, lddw = _matrix(dw, "dw", "float32", p.f, c, dev)
+    _ck(lib().gcnsa_op_gemm_packed8(stream, n, p.f, c, p.on("p", n, p.f, dev), gp, ldg, dwp, lddw, accumulate,
+                                    *_bytes_of(workspace, "workspace", dev)))
 
 
 def op_gemm_packed8_workspace(n, f, c) -> int:
@@ -877,17 +896,14 @@ def op_gemm_packed8_workspace(n, f, c) -> int:
 def op_linear_ce(h, d, w, c, y, n_train, loss, dh=None, dw=None, db=None, bias=None, mask=None, accumulate=0, workspace=None):
     """Loss of the output layer z = h w + bias under masked softmax cross-entropy, and the gradients asked for (see
     include/gcnsa.h); n_train is the number of masked rows."""
-    n = _rows_of(h, "h")
-    hp, ldh = _operand(h, "h", "float32", n, d)
-    wp, ldw = _operand(w, "w", "float32", d, c, h)
-    dhp, lddh = _operand(dh, "dh", "float32", n, d, h)
-    dwp, lddw = _operand(dw, "dw", "float32", d, c, h)
-    yp, mp = _operand(y, "y", "int32", n, None, h)[0], _operand(mask, "mask", "uint8", n, None, h)[0]
-    vec = [_operand(t, nm, "float32", k, None, h)[0] for t, nm, k in ((bias, "bias", c), (loss, "loss", 1), (db, "db", c))]
-    if workspace is not None:
-        _operand(workspace, "workspace", str(workspace.dtype)[6:], 0, None, h)
-    _ck(lib().gcnsa_op_linear_ce(_on(h), n, d, c, hp, ldh, wp, ldw, vec[0], yp, mp, n_train, vec[1], dhp, lddh, dwp, lddw, vec[2],
-                                 accumulate, _dp(workspace), _nbytes(workspace)))
+    n, dev, stream = _leader(h, "h")
+    hp, ldh = _matrix(h, "h", "float32", n, d, dev)
+    wp, ldw = _matrix(w, "w", "float32", d, c, dev)
+    dhp, lddh = _matrix(dh, "dh", "float32", n, d, dev)
+    dwp, lddw = _matrix(dw, "dw", "float32", d, c, dev)
+    _ck(lib().gcnsa_op_linear_ce(stream, n, d, c, hp, ldh, wp, ldw, _vector(bias, "bias", "float32", c, dev), _vector(y, "y", "int32", n, dev),
+                                 _vector(mask, "mask", "uint8", n, dev), n_train, _vector(loss, "loss", "float32", 1, dev), dhp, lddh, dwp,
+                                 lddw, _vector(db, "db", "float32", c, dev), accumulate, *_bytes_of(workspace, "workspace", dev)))
 
 
 def op_linear_ce_workspace(n, d, c) -> int:
