@@ -667,7 +667,7 @@ int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float
                                  int32_t accumulate, void* scratch, size_t scratch_bytes);
 size_t gcnsa_op_layer_norm_backward_scratch(int64_t n, int32_t f);
 
-/* Make a checkpoint of x, and restore one. */
+/* Make a checkpoint of x, and restore one.  n < 2^31. */
 int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p);
 int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx);
 

@@ -1656,7 +1656,7 @@ int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float
 }
 
 int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p) {
-  if (n < 0 || f < 1) return fail(GCNSA_ERR_ARG, "negative dimension or f < 1");
+  if (n < 0 || f < 1 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension or f < 1");
   if (n == 0) return GCNSA_OK;
   if (!x || !p) return fail(GCNSA_ERR_ARG, "NULL pointer");
   if (ldx < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");
@@ -1666,7 +1666,7 @@ int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t l
 }
 
 int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx) {
-  if (n < 0 || f < 1) return fail(GCNSA_ERR_ARG, "negative dimension or f < 1");
+  if (n < 0 || f < 1 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension or f < 1");
   if (n == 0) return GCNSA_OK;
   if (!x || !p) return fail(GCNSA_ERR_ARG, "NULL pointer");
   if (ldx < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");

@@ -111,11 +111,10 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
       const uint32_t ex = pack8_exponent(m);
-      const float inv = pack8_inverse(ex);
-      uint32_t b[4];
+      float b[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) b[k] = pack8_round(c + k < f && ex != 255 ? x[4 * v + k] : 0.f, inv);
-      if (in && c < f16) *reinterpret_cast<uint32_t*>(q + c) = pack8_join(b[0], b[1], b[2], b[3]);
+      for (int k = 0; k < 4; ++k) b[k] = c + k < f && ex != 255 ? x[4 * v + k] : 0.f;
+      if (in && c < f16) *reinterpret_cast<uint32_t*>(q + c) = pack8_bytes(b, ex);
       if (in && c < f && (t & 7) == 0) e[c / kPackBlock] = (uint8_t)ex;
     } else {  // a warp holds a block
 #pragma unroll
@@ -123,7 +122,8 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
         const int c = (4 * v + k) * T + t;
         const float a = c < f ? x[4 * v + k] : 0.f;
         const uint32_t ex = pack8_exponent(__reduce_max_sync(kFull, __float_as_uint(a) & 0x7fffffffu));
-        if (in && c < f16) q[c] = (int8_t)pack8_round(ex == 255 ? 0.f : a, pack8_inverse(ex));
+        const float b[4] = {ex == 255 ? 0.f : a, 0.f, 0.f, 0.f};
+        if (in && c < f16) q[c] = (int8_t)pack8_bytes(b, ex);
         if (in && c < f && (t & 31) == 0) e[c / kPackBlock] = (uint8_t)ex;
       }
     }
@@ -188,6 +188,16 @@ __device__ __forceinline__ void team_sum(float (&v)[COUNT], float (*sh)[COUNT][k
 // y = ((x - mean) rstd) gamma + beta, then ReLU; a NaN stays one
 __device__ __forceinline__ float norm_value(float xh, float gamma, float beta) { return fmaf(xh, gamma, beta); }
 
+// gamma or beta of a thread's columns, kept in registers from row to row (`none` where the pointer is NULL)
+template <int T, int NV, bool VEC>
+__device__ __forceinline__ void load_cols(const float* __restrict__ w, float none, int f, int t, float (&o)[4 * NV]) {
+#pragma unroll
+  for (int i = 0; i < 4 * NV; ++i) {
+    const int c = col_of<T, VEC>(i / 4, i % 4, t);
+    o[i] = w && c < f ? __ldg(w + c) : none;
+  }
+}
+
 // The mean is corrected by the mean of what is left after subtracting it, and the variance is taken around the corrected
 // one: a column offset of 1e4 next to a spread of 1 then costs no digits, as the differences x - mean are exact.
 template <int T, int NV, bool VEC>
@@ -202,6 +212,9 @@ layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __re
   const int n_pad = (int)min(ldy, (int64_t)((f + 3) / 4 * 4));
   const float inv_f = 1.f / (float)f;
   int s1 = 0, s2 = 0;
+  float ga[4 * NV], be[4 * NV];
+  load_cols<T, NV, VEC>(gamma, 1.f, f, t, ga);
+  load_cols<T, NV, VEC>(beta, 0.f, f, t, be);
   // all lanes of a warp stay together (shuffles): rows past the end are computed on zeros and not written
   for (int64_t base = (int64_t)blockIdx.x * TEAMS; base < n; base += (int64_t)gridDim.x * TEAMS) {
     const int64_t row = base + team;
@@ -226,13 +239,10 @@ layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __re
     // (max drops a NaN, which has to reach rstd)
     const float var = fmaf(-dm, dm, d[1] * inv_f), r = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int i = 0; i < 4 * NV; ++i) a[i] = norm_value((a[i] - dm) * r, ga[i], be[i]);
+    if (relu)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = col_of<T, VEC>(v, k, t);
-        const float o = norm_value((a[4 * v + k] - dm) * r, gamma && c < f ? __ldg(gamma + c) : 1.f, beta && c < f ? __ldg(beta + c) : 0.f);
-        a[4 * v + k] = relu && o < 0.f ? 0.f : o;
-      }
+      for (int i = 0; i < 4 * NV; ++i) a[i] = a[i] < 0.f ? 0.f : a[i];
     if (y8.q) store_packed<T, NV, VEC>(y8, row, in, f, t, a);
     if (bits.w) store_bits<T, NV, VEC>(bits, row, in, f, t, a);
     if (in) {
@@ -246,17 +256,25 @@ layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __re
 }
 
 // Where v = xh gamma + beta lies within its own rounding error of zero the sign is taken in 64 bits: a gradient is kept or
-// dropped by it.  (xh is off by 3 and v by one more half unit of 2^-23.)
+// dropped by it.  xh is off by 3 half units of 2^-23 and v by one more: by at most 2.4e-7 (|xh gamma| + |v|), and as |xh gamma|
+// <= |v| + |beta| its sign is certain where |v| is above 2.5e-7 |beta|.
+__device__ __forceinline__ bool near_zero(float v, float beta) { return !(fabsf(v) > 1e-6f * fabsf(beta)); }
+__device__ __forceinline__ bool exactly_positive(float x, float mean, float rstd, float gamma, float beta) {
+  return ((double)x - mean) * rstd * gamma + beta > 0.0;
+}
 __device__ __forceinline__ bool norm_positive(float x, float mean, float rstd, float xh, float gamma, float beta) {
   const float v = fmaf(xh, gamma, beta);
-  if (fabsf(v) > 4.8e-7f * (fabsf(xh * gamma) + fabsf(beta))) return v > 0.f;
-  return ((double)x - mean) * rstd * gamma + beta > 0.0;
+  return near_zero(v, beta) ? exactly_positive(x, mean, rstd, gamma, beta) : v > 0.f;
 }
 
 // dx = rstd (u - mean(u) - xh mean(u xh)), u = g gamma where the ReLU let the value through; every block leaves the column
 // sums of g xh and g over its rows in its row of `partial` (2 f floats), which norm_sums adds in block order.
+//
+// Registers decide how many rows are on the way: with 127 a thread (the compiler's choice for NV = 2) two blocks an SM, 269 498 x
+// 256 takes 158 us; at most 80 make it three, 148.  (The next row's loads before this row's sums: 156, with spills 214.)
+constexpr int grad_blocks_per_sm(int nv) { return nv <= 1 ? 4 : nv <= 2 ? 3 : nv <= 4 ? 2 : 1; }
 template <int T, int NV, bool VEC, bool X8>
-__global__ void __launch_bounds__(kNormThreads)
+__global__ void __launch_bounds__(kNormThreads, grad_blocks_per_sm(NV))
 layer_norm_grad(int64_t n, int f, const float* g, int64_t ldg, const float* x, int64_t ldx, PackedRows x8,
                 const float* __restrict__ mean, const float* __restrict__ rstd, const float* __restrict__ gamma,
                 const float* __restrict__ beta, int relu, BitRows bits, float* dx, int64_t lddx,
@@ -272,6 +290,9 @@ layer_norm_grad(int64_t n, int f, const float* g, int64_t ldg, const float* x, i
   float dg[4 * NV], db[4 * NV];
 #pragma unroll
   for (int i = 0; i < 4 * NV; ++i) dg[i] = db[i] = 0.f;
+  float ga[4 * NV], be[4 * NV];
+  load_cols<T, NV, VEC>(gamma, 1.f, f, t, ga);
+  load_cols<T, NV, VEC>(beta, 0.f, f, t, be);
   for (int64_t base = (int64_t)blockIdx.x * TEAMS; base < n; base += (int64_t)gridDim.x * TEAMS) {
     const int64_t row = base + team;
     const bool in = row < n;
@@ -280,23 +301,45 @@ layer_norm_grad(int64_t n, int f, const float* g, int64_t ldg, const float* x, i
     else load_row<T, NV, VEC>(x + row * ldx, in ? f : 0, t, a);
     load_row<T, NV, VEC>(g + row * ldg, in ? f : 0, t, u);
     const float mu = in ? mean[row] : 0.f, r = in ? rstd[row] : 0.f;
+    if (relu) {
+      if (bits.w) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int c0 = col_of<T, VEC>(v, 0, t);
+          const uint32_t word = VEC && in && c0 < f ? bits.w[row * bits.ld + c0 / 32] >> (c0 & 31) : 0u;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int c = col_of<T, VEC>(v, k, t);
+            const bool keep = VEC ? (word >> k) & 1u : in && c < f && bit_at(bits, row, c);
+            u[4 * v + k] = keep ? u[4 * v + k] : 0.f;
+          }
+        }
+      } else {
+        bool close = false;
+#pragma unroll
+        for (int i = 0; i < 4 * NV; ++i) {
+          const float v = fmaf((a[i] - mu) * r, ga[i], be[i]);
+          const bool zero = near_zero(v, be[i]);
+          close |= zero;
+          u[i] = zero || v > 0.f ? u[i] : 0.f;
+        }
+        if (close)
+#pragma unroll
+          for (int i = 0; i < 4 * NV; ++i)
+            if (near_zero(fmaf((a[i] - mu) * r, ga[i], be[i]), be[i]) && !exactly_positive(a[i], mu, r, ga[i], be[i])) u[i] = 0.f;
+      }
+    }
+    // (columns past the end: u is 0, and what xh is there enters nothing that is written)
     float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int i = 4 * v + k, c = col_of<T, VEC>(v, k, t);
-        const bool col_in = in && c < f;
-        const float ga = gamma && c < f ? __ldg(gamma + c) : 1.f;
-        const float xh = col_in ? (a[i] - mu) * r : 0.f;
-        if (relu && col_in && !(bits.w ? bit_at(bits, row, c) : norm_positive(a[i], mu, r, xh, ga, beta ? __ldg(beta + c) : 0.f))) u[i] = 0.f;
-        a[i] = xh;
-        dg[i] = fmaf(u[i], xh, dg[i]);
-        db[i] += u[i];
-        u[i] *= ga;
-        s[0] += u[i];
-        s[1] = fmaf(u[i], xh, s[1]);
-      }
+    for (int i = 0; i < 4 * NV; ++i) {
+      a[i] = (a[i] - mu) * r;
+      dg[i] = fmaf(u[i], a[i], dg[i]);
+      db[i] += u[i];
+      u[i] *= ga[i];
+      s[0] += u[i];
+      s[1] = fmaf(u[i], a[i], s[1]);
+    }
     team_sum<T, 2>(s, sh2, s2);
     const float c1 = s[0] * inv_f, c2 = s[1] * inv_f;
 #pragma unroll
@@ -514,11 +557,13 @@ norm_sums(int f, int blocks, const float* __restrict__ partial, float* __restric
 }
 
 // ---- checkpoints: eight lanes to a block, four blocks of any rows to a warp at a time --------------------------------
-constexpr int kPackUnroll = 4;
-struct BlockWalk {  // (row, block of the row) of a lane's blocks, one grid stride after the other
-  int64_t row, drow;
+// (row, block of the row) of a lane's blocks, one grid stride after the other.  A row is 32 bits, so that its place costs two
+// multiplications.
+struct BlockWalk {
+  uint32_t row, drow;
   int b, db, nb;
-  __device__ __forceinline__ BlockWalk(int nb_, int64_t first, int64_t stride) : row(first / nb_), drow(stride / nb_), b((int)(first % nb_)), db((int)(stride % nb_)), nb(nb_) {}
+  __device__ __forceinline__ BlockWalk(int nb_, uint64_t first, uint64_t stride)
+      : row((uint32_t)(first / nb_)), drow((uint32_t)(stride / nb_)), b((int)(first % nb_)), db((int)(stride % nb_)), nb(nb_) {}
   __device__ __forceinline__ void next() {
     row += drow;
     b += db;
@@ -528,81 +573,80 @@ struct BlockWalk {  // (row, block of the row) of a lane's blocks, one grid stri
     }
   }
 };
-template <bool VEC>
+// UNROLL blocks of a lane are on the way at a time; reading bytes takes twice as many of them to fill the time to memory.
+template <bool VEC, int UNROLL>
 __global__ void __launch_bounds__(256)
-pack8_rows(int64_t n, int f, int nb, const float* __restrict__ x, int64_t ldx, PackedRows p) {
+pack8_rows(uint32_t n, int f, int nb, const float* __restrict__ x, int64_t ldx, PackedRows p) {
   wait_for_predecessors();
   const int g = threadIdx.x & 7, f16 = (f + 15) / 16 * 16;
-  BlockWalk at(nb, ((int64_t)blockIdx.x * 256 + threadIdx.x) / 8, (int64_t)gridDim.x * 32);
-  // (a warp's four groups run on together until the first of them is past the end)
+  BlockWalk at(nb, ((uint64_t)blockIdx.x * 256 + threadIdx.x) / 8, (uint64_t)gridDim.x * 32);
+  // (a warp's four groups run on together until the last of them is past the end)
   while (__any_sync(kFull, at.row < n)) {
-    float a[kPackUnroll][4];
-    int64_t rows[kPackUnroll];
-    int blk[kPackUnroll];
+    float a[UNROLL][4];
+    BlockWalk to = at;
 #pragma unroll
-    for (int i = 0; i < kPackUnroll; ++i) {
-      rows[i] = at.row;
-      blk[i] = at.b;
+    for (int i = 0; i < UNROLL; ++i) {
       const int c = 32 * at.b + 4 * g;
-      const bool in = at.row < n;
+      const float* src = x + at.row * ldx + c;
       if constexpr (VEC) {
-        const float4 v = in && c < f ? *reinterpret_cast<const float4*>(x + at.row * ldx + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        a[i][0] = v.x;
-        a[i][1] = c + 1 < f ? v.y : 0.f;
-        a[i][2] = c + 2 < f ? v.z : 0.f;
-        a[i][3] = c + 3 < f ? v.w : 0.f;
+        const float4 v = at.row < n && c < f ? __ldg(reinterpret_cast<const float4*>(src)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        a[i][0] = v.x; a[i][1] = v.y; a[i][2] = v.z; a[i][3] = v.w;
+        if (c + 3 >= f)
+#pragma unroll
+          for (int k = 1; k < 4; ++k) a[i][k] = c + k < f ? a[i][k] : 0.f;
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) a[i][k] = in && c + k < f ? x[at.row * ldx + c + k] : 0.f;
+        for (int k = 0; k < 4; ++k) a[i][k] = at.row < n && c + k < f ? __ldg(src + k) : 0.f;
       }
       at.next();
     }
 #pragma unroll
-    for (int i = 0; i < kPackUnroll; ++i) {
+    for (int i = 0; i < UNROLL; ++i) {
       uint32_t m = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) m = max(m, __float_as_uint(a[i][k]) & 0x7fffffffu);
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
       const uint32_t ex = pack8_exponent(m);
-      const float inv = pack8_inverse(ex);
-      uint32_t b[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) b[k] = pack8_round(ex == 255 ? 0.f : a[i][k], inv);
-      const int c = 32 * blk[i] + 4 * g;
-      if (rows[i] < n) {
-        if (c < f16) *reinterpret_cast<uint32_t*>(p.q + rows[i] * p.ldq + c) = pack8_join(b[0], b[1], b[2], b[3]);
-        if (g == 0) p.e[rows[i] * p.lde + blk[i]] = (uint8_t)ex;
+      if (ex == 255) a[i][0] = a[i][1] = a[i][2] = a[i][3] = 0.f;
+      const int c = 32 * to.b + 4 * g;
+      if (to.row < n) {
+        if (c < f16) *reinterpret_cast<uint32_t*>(p.q + to.row * p.ldq + c) = pack8_bytes(a[i], ex);
+        if (g == 0) p.e[to.row * p.lde + to.b] = (uint8_t)ex;
       }
+      to.next();
     }
   }
 }
-template <bool VEC>
+template <bool VEC, int UNROLL>
 __global__ void __launch_bounds__(256)
-unpack8_rows(int64_t n, int f, int nb, PackedRows p, float* __restrict__ x, int64_t ldx) {
+unpack8_rows(uint32_t n, int f, int nb, PackedRows p, float* __restrict__ x, int64_t ldx) {
   wait_for_predecessors();
   const int g = threadIdx.x & 7, n_pad = (int)min(ldx, (int64_t)f + (4 - f % 4) % 4);
-  BlockWalk at(nb, ((int64_t)blockIdx.x * 256 + threadIdx.x) / 8, (int64_t)gridDim.x * 32);
+  BlockWalk at(nb, ((uint64_t)blockIdx.x * 256 + threadIdx.x) / 8, (uint64_t)gridDim.x * 32);
   while (at.row < n) {
-    uint32_t q[kPackUnroll], ex[kPackUnroll];
+    uint32_t q[UNROLL], ex[UNROLL];
     BlockWalk to = at;
 #pragma unroll
-    for (int i = 0; i < kPackUnroll; ++i) {
+    for (int i = 0; i < UNROLL; ++i) {
       const int c = 32 * at.b + 4 * g;
       const bool in = at.row < n && c < f;
-      q[i] = in ? *reinterpret_cast<const uint32_t*>(p.q + at.row * p.ldq + c) : 0u;
-      ex[i] = in ? p.e[at.row * p.lde + at.b] : 0u;
+      q[i] = in ? __ldg(reinterpret_cast<const uint32_t*>(p.q + at.row * p.ldq + c)) : 0u;
+      ex[i] = in ? __ldg(p.e + at.row * p.lde + at.b) : 0u;
       at.next();
     }
 #pragma unroll
-    for (int i = 0; i < kPackUnroll; ++i) {
+    for (int i = 0; i < UNROLL; ++i) {
       const int c = 32 * to.b + 4 * g;
       if (to.row < n && c < f) {
         float a[4];
         pack8_open(q[i], a);
         const float step = pack8_step(ex[i]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] = c + k < f ? a[k] * step : 0.f;
+        for (int k = 0; k < 4; ++k) a[k] *= step;
+        if (c + 3 >= f)
+#pragma unroll
+          for (int k = 1; k < 4; ++k) a[k] = c + k < f ? a[k] : 0.f;
         float* dst = x + to.row * ldx + c;
         if constexpr (VEC) {
           *reinterpret_cast<float4*>(dst) = make_float4(a[0], a[1], a[2], a[3]);
@@ -624,7 +668,9 @@ PackedRows rows_of(const gcnsa_packed8* p) {
 // blocks of a kernel whose teams take a row at a time
 int norm_blocks(int64_t n, int teams, int most) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + teams - 1) / teams, most)); }
 int grad_teams(int32_t f) { return f <= kNarrowCols ? kNormThreads : f <= 32 ? 32 : f <= 64 ? 16 : f <= 512 ? 8 : 1; }
-int grad_blocks(int64_t n, int32_t f) { return norm_blocks(n, grad_teams(f), 148 * 4); }
+// (float4 of a row to a thread, as launch_layer_norm_grad has it)
+int grad_nv(int32_t f) { return f <= 128 ? 1 : f <= 256 ? 2 : f <= 512 ? 4 : f <= 1024 ? 1 : f <= 2048 ? 2 : f <= 4096 ? 4 : 8; }
+int grad_blocks(int64_t n, int32_t f) { return norm_blocks(n, grad_teams(f), 148 * (f > kNormMaxCols ? 4 : grad_blocks_per_sm(grad_nv(f)))); }
 
 }  // namespace
 
@@ -696,22 +742,23 @@ int launch_layer_norm_grad(void* stream, int64_t n, int32_t f, const float* g, i
   return (int)cudaGetLastError();
 }
 
-static int pack_blocks(int64_t groups) { return (int)std::max<int64_t>(1, std::min<int64_t>((groups + 32 * kPackUnroll - 1) / (32 * kPackUnroll), 148 * 8)); }
+constexpr int kPackUnroll = 4, kUnpackUnroll = 8;
+static int pack_blocks(int64_t groups, int unroll) { return (int)std::max<int64_t>(1, std::min<int64_t>((groups + 32 * unroll - 1) / (32 * unroll), 148 * 8)); }
 
 int launch_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p) {
   if (n <= 0) return 0;
-  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb);
-  if (vec_rows(x, ldx)) launch(pack8_rows<true>, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, x, ldx, rows_of(p));
-  else launch(pack8_rows<false>, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, x, ldx, rows_of(p));
+  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb, kPackUnroll);
+  auto run = [&](auto kernel) { launch(kernel, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, x, ldx, rows_of(p)); };
+  vec_rows(x, ldx) ? run(pack8_rows<true, kPackUnroll>) : run(pack8_rows<false, kPackUnroll>);
   note_launch();
   return (int)cudaGetLastError();
 }
 
 int launch_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx) {
   if (n <= 0) return 0;
-  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb);
-  if (vec_rows(x, ldx)) launch(unpack8_rows<true>, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, rows_of(p), x, ldx);
-  else launch(unpack8_rows<false>, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, rows_of(p), x, ldx);
+  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb, kUnpackUnroll);
+  auto run = [&](auto kernel) { launch(kernel, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, rows_of(p), x, ldx); };
+  vec_rows(x, ldx) ? run(unpack8_rows<true, kUnpackUnroll>) : run(unpack8_rows<false, kUnpackUnroll>);
   note_launch();
   return (int)cudaGetLastError();
 }

@@ -17,22 +17,26 @@ constexpr int kPackBlock = 32;
 // bits: the largest of the block's magnitudes as fp32 words with the sign cleared (as integers these order like the values,
 // infinity and NaN last)
 __device__ __forceinline__ uint32_t pack8_exponent(uint32_t bits) {
-  const uint32_t ex = bits >> 23, mant = bits & 0x7fffffu;
-  if (ex == 255) return 255;
-  // 2^(ex - 133) puts the value at 64 to 128 steps; from 127.5 on (mantissa 1.9921875) it would round to 128
-  if (ex < 7) return 1;
-  return min(ex - 6 + (mant >= 0x7f0000u ? 1u : 0u), 248u);
+  if (bits >= 0x7f800000u) return 255;
+  // 2^(exponent - 133) puts the value at 64 to 128 steps; from 127.5 on (mantissa 1.9921875, 0x10000 below the next exponent) it
+  // would round to 128
+  return (uint32_t)min(max((int)((bits + 0x10000u) >> 23) - 6, 1), 248);
 }
 // 1 / step; 0 for a block that is not finite
 __device__ __forceinline__ float pack8_inverse(uint32_t e) { return e == 255 ? 0.f : __uint_as_float((254 - e) << 23); }
 __device__ __forceinline__ float pack8_step(uint32_t e) { return __uint_as_float(e << 23); }
-// rint(x * inv) as the low byte of the sum's mantissa (x * inv is exact and below 128; ties to even).  x is 0 where the block
-// is not finite.
-__device__ __forceinline__ uint32_t pack8_round(float x, float inv) {
-  return __float_as_uint(fminf(fmaxf(x * inv, -127.f), 127.f) + 12582912.f);
-}
-__device__ __forceinline__ uint32_t pack8_join(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+// Four values as bytes: rint(x * inv) is the low byte of x * inv + 1.5 2^23 (x * inv is exact and below 128; ties to even).  x is 0
+// where the block is not finite.
+__device__ __forceinline__ uint32_t pack8_bytes(const float (&x)[4], uint32_t e) {
+  const float inv = pack8_inverse(e);
+  uint32_t b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float s = x[k] * inv;
+    if (e == 248) s = fminf(fmaxf(s, -127.f), 127.f);
+    b[k] = __float_as_uint(s + 12582912.f);
+  }
+  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 // four packed bytes as floats: 2^23 + (q + 128) has q + 128 as its low byte
 __device__ __forceinline__ void pack8_open(uint32_t q4, float (&v)[4]) {
