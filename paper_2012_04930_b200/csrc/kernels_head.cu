@@ -7,7 +7,7 @@
 // results, written transposed, are dH and dW.  db falls out of the second one, whose left operand passes through registers.
 //  - c <= 128: a tile holds whole rows of z, so softmax, loss and G come from one pass over the products.
 //  - c > 128: one pass keeps a running maximum and sum of exponentials per row (8 bytes per row and run of tiles), then, a
-//    piece of the classes at a time, z is made again and turned into G.  A piece is as large as keeps G^T in L2.  Rows that
+//    piece of the classes at a time, z is made again and turned into G.  Rows that
 //    do not count are left out of all products: the others are gathered first.
 // The two gradient products of a piece are independent and run as one launch, the slices of dW^T before the tiles of dH^T.
 #include <cuda_runtime.h>
@@ -271,7 +271,9 @@ int launch_add_slices(cudaStream_t s, int64_t rows, int64_t n, int slices, const
 
 // ---- plan of a call: sizes that hold for every count of rows up to n -------------------------------------------------
 constexpr int kWholeCols = 128;                    // classes that one tile holds
-constexpr int64_t kPieceFloats = int64_t(16) << 20;  // of G^T: half of L2
+// Floats of G^T at most (a piece has 128 classes at least): 160 MB.  Three launches a piece cost about 30 us on top of their work, more than
+// it costs that G^T is then read from HBM in part: 20 011 x 256 x 10 007 with 64 / 96 / 192 MB 1 922 / 1 793 / 1 722 us.
+constexpr int64_t kPieceFloats = int64_t(40) << 20;
 struct CePlan {
   int64_t gt_floats, partial_floats, sums_floats, slots;
   size_t gt, partial, sums, hc, wc, yc, rows, place, counts, total, zy, lse, row_loss, part, losses, end;
@@ -305,15 +307,15 @@ CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   p.end = at;
   return p;
 }
-// Classes of a piece: a multiple of 128 whose G^T fits its room, and from the upper half of those the one whose tiles fill
-// the rounds over the SMs best.
-int64_t piece_classes(const CePlan& p, int64_t rows, int32_t c) {
+// Classes of a piece: the multiple of 128 whose G^T fits its room and with which the rounds of z's tiles over the SMs and the
+// launches (about 30 k-blocks' time a piece) cost least.
+int64_t piece_classes(const CePlan& p, int64_t rows, int32_t d, int32_t c) {
   const int64_t all = div_up(c, 128), most = std::max<int64_t>(1, std::min(all, p.gt_floats / (128 * up4(rows)))), tiles_m = div_up(rows, BM), sms = sm_count();
-  int64_t best = most;
-  double best_cost = 1e30;
+  int64_t best = most, best_cost = INT64_MAX;
   for (int64_t k = most; k >= std::max<int64_t>(1, most / 2); --k) {
-    const double cost = (double)div_up(tiles_m * k, sms) / (double)k;
-    if (cost < best_cost - 1e-9) {
+    const int64_t pieces = div_up(all, k), last = all - (pieces - 1) * k;
+    const int64_t cost = ((pieces - 1) * div_up(tiles_m * k, sms) + div_up(tiles_m * last, sms)) * (div_up(d, BK) + 2) + pieces * 30;
+    if (cost < best_cost) {
       best = k;
       best_cost = cost;
     }
@@ -464,7 +466,7 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
       GCNSA_STEP(launch_add_slices(s, a.dw ? a.d : 0, a.c, 0, nullptr, up4(a.c), a.dw, a.lddw, a.dw ? std::min<int64_t>(a.lddw, up4(a.c)) : a.c, 0, nullptr, a.db, a.accumulate));
     return 0;
   }
-  const int64_t piece = whole ? a.c : piece_classes(pl, R, a.c);
+  const int64_t piece = whole ? a.c : piece_classes(pl, R, a.d, a.c);
   for (int64_t c0 = 0; c0 < a.c; c0 += piece) {
     const int64_t width = std::min<int64_t>(piece, a.c - c0);
     if (!whole) {

@@ -40,7 +40,7 @@ constexpr int kAWarp0 = 4, kBWarp0 = 12, kSplitGroups = 2, kFoldWarp0 = 20, kFol
 // registers per thread by role, in multiples of 8; their sum over the seven warpgroups is at most what the launch gives (72 each)
 constexpr int kRegsIssue = 32, kRegsA = 72, kRegsB = 64, kRegsFold = 96;
 static_assert(kRegsIssue + kSplitGroups * (kRegsA + kRegsB) + 2 * kRegsFold <= 7 * 72, "setmaxnreg draws on the registers of the launch");
-constexpr int kSmallFolds = 8;
+constexpr int kSmallFolds = 8, kRetired = 8;
 constexpr int A_SLOT = BM * BK * 4;
 
 // A: K-major (k contiguous in memory), MN-major (rows of D contiguous), or MN-major without the alignment that TMA needs
@@ -201,9 +201,9 @@ struct TermShape {
   static constexpr int NEED = BAR_OFF + 512 + 1024;
   static constexpr int SMEM_BYTES = NEED > 118 * 1024 ? NEED : 118 * 1024;
   static_assert(NA % kSplitGroups == 0 && NB % kSplitGroups == 0, "a slot belongs to one group");
-  // Stages of terms are not: a group's wait for the MMAs of k-block g - NS is told from the phase before the last, k-block
-  // g - 2 NS, by the group's own last wait, for k-block g - kSplitGroups - NS.
-  static_assert(NSA >= kSplitGroups && NSB >= kSplitGroups, "the phase before the last of a stage has ended");
+  // A group that waits for the MMAs of k-block g - NS has seen those of g - kSplitGroups - NS retire, so the phase before the
+  // last of that barrier, k-block g - NS - kRetired, has ended.
+  static_assert(kRetired >= kSplitGroups, "the phase before the last of a retire barrier has ended");
   static_assert(A_COL0 + NSA * A_COLS <= TMEM_COLS, "tensor memory has 512 columns");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
 };
@@ -299,9 +299,8 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
   uint64_t* free_b = full_b + NB;
   uint64_t* ready_a = free_b + NB;        // [NSA] terms in place
   uint64_t* ready_b = ready_a + NSA;      // [NSB]
-  uint64_t* empty_a = ready_b + NSB;      // [NSA] MMAs of the stage retired
-  uint64_t* empty_b = empty_a + NSA;      // [NSB]
-  uint64_t* acc_full = empty_b + NSB;     // [2]
+  uint64_t* retired = ready_b + NSB;      // [kRetired] MMAs of k-block g have read their operands: barrier g % kRetired
+  uint64_t* acc_full = retired + kRetired;  // [2]
   uint64_t* acc_empty = acc_full + 2;     // [2] read back by the fold warps
   uint64_t* small_empty = acc_empty + 2;
   uint64_t* pair = small_empty + 1;       // [4] the two fold warps of a lane quarter (Out::whole)
@@ -328,12 +327,9 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
     }
     for (int i = 0; i < NSB; ++i) {
       mbar_init(&ready_b[i], 4);
-      mbar_init(&empty_b[i], 1);
     }
-    for (int i = 0; i < NSA; ++i) {
-      mbar_init(&ready_a[i], 4);
-      mbar_init(&empty_a[i], 1);
-    }
+    for (int i = 0; i < NSA; ++i) mbar_init(&ready_a[i], 4);
+    for (int i = 0; i < kRetired; ++i) mbar_init(&retired[i], 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
       mbar_init(&acc_empty[i], kFoldWarps);
@@ -420,9 +416,12 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         for (int it = 0; it < wk.n_kb; ++it, ++g) {
           const uint32_t sa = g % NSA, pa = (g / NSA) & 1, sb = g % NSB, pb = (g / NSB) & 1;
           const int in_fold = it % S::FOLD, in_small = it % (S::FOLD * kSmallFolds);
+          // (the questions are asked at once, their answers take 30 clocks each; only a no leads to a wait)
+          const bool have_b = mbar_try_wait(&ready_b[sb], pb), have_a = mbar_try_wait(&ready_a[sa], pa);
           if (in_fold == 0) ok = mbar_wait(&acc_empty[folds & 1], ((folds >> 1) & 1) ^ 1, 46);
           if (S::SMALL && ok && in_small == 0) ok = mbar_wait(small_empty, (smalls & 1) ^ 1, 47);
-          ok = ok && mbar_wait(&ready_b[sb], pb, 43) && mbar_wait(&ready_a[sa], pa, 52);
+          if (!have_b) ok = ok && mbar_wait(&ready_b[sb], pb, 43);
+          if (!have_a) ok = ok && mbar_wait(&ready_a[sa], pa, 52);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -446,8 +445,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
               umma_bf16_ta(d_small, a1, bk, idesc, 1);
               umma_bf16_ta(d_main, a0, bk, idesc, !S::SMALL || kk != 0 || in_fold != 0);
             }
-            umma_commit(&empty_a[sa]);  // arrive when the MMAs above have read their operands
-            umma_commit(&empty_b[sb]);
+            umma_commit(&retired[g % kRetired]);  // arrives when the MMAs above have read their operands
             if (last_fold) umma_commit(&acc_full[folds & 1]);
           }
           __syncwarp();
@@ -515,7 +513,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
 #pragma unroll
         for (int k = 0; k < 16; ++k) split3(x[2 * k], x[2 * k + 1], t0[k], t1[k], t2[k]);
         const uint32_t sa = g % NSA;
-        ok = __all_sync(0xffffffffu, mbar_wait_long(&empty_a[sa], ((g / NSA) & 1) ^ 1, 49));
+        if (g >= NSA) ok = __all_sync(0xffffffffu, mbar_wait(&retired[(g - NSA) % kRetired], ((g - NSA) / kRetired) & 1, 49));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t ta = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(S::A_COL0 + sa * S::A_COLS);
@@ -566,7 +564,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         if (!ok) break;
         TermB<S> tb;
         tb.load(smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane);
-        ok = __all_sync(0xffffffffu, mbar_wait_long(&empty_b[sb], ((g / NSB) & 1) ^ 1, 45));
+        if (g >= NSB) ok = __all_sync(0xffffffffu, mbar_wait(&retired[(g - NSB) % kRetired], ((g - NSB) / kRetired) & 1, 45));
         if (!ok) break;
         tb.store(smem + S::T_OFF + sb * NTB * S::B_TERM, q, lane, e8);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the MMA
@@ -705,11 +703,11 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
 #pragma unroll
             for (int j = 0; j < HALF; ++j) sum[j] -= j == label ? 1.f : 0.f;
           if (row_in) {
-            float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
             const int64_t ldg = args.ce.ldg;
+            float* at = args.ce.gt + nb * ldg + m;
 #pragma unroll
-            for (int j = 0; j < HALF; ++j)
-              if (j < cols) gt[j * ldg] = sum[j] * scale;
+            for (int j = 0; j < HALF; ++j, at += ldg)
+              if (j < cols) *at = sum[j] * scale;
           }
         } else {
           float mx = -INFINITY, zy = 0.f;
@@ -760,11 +758,11 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
               if (here || (half == 0 && (label + c0 < 0 || label + c0 >= p.N)))  // (a label outside: no logit)
                 args.ce.row_loss[m] = !on ? 0.f : here ? (base + logf(s)) - zy : NAN;
               if (args.ce.gt) {
-                float* gt = args.ce.gt + (int64_t)nb * args.ce.ldg + m;
                 const int64_t ldg = args.ce.ldg;
+                float* at = args.ce.gt + nb * ldg + m;
 #pragma unroll
-                for (int j = 0; j < HALF; ++j)
-                  if (j < cols) gt[j * ldg] = on ? (sum[j] * inv - (j == label ? 1.f : 0.f)) * args.ce.inv_nt : 0.f;
+                for (int j = 0; j < HALF; ++j, at += ldg)
+                  if (j < cols) *at = on ? (sum[j] * inv - (j == label ? 1.f : 0.f)) * args.ce.inv_nt : 0.f;
               }
             }
           }
