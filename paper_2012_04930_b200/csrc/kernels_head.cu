@@ -270,6 +270,7 @@ int launch_add_slices(cudaStream_t s, int64_t rows, int64_t n, int slices, const
 }
 
 // ---- plan of a call: sizes that hold for every count of rows up to n -------------------------------------------------
+constexpr int kSumLines = TermShape<128, ASrc::kMajor, false, Out::transposed>::AG;  // of a_sums, per slice
 constexpr int kWholeCols = 128;                    // classes that one tile holds
 // Floats of G^T at most (a piece has 128 classes at least): 160 MB.  Three launches a piece cost about 30 us on top of their work, more than
 // it costs that G^T is then read from HBM in part: 20 011 x 256 x 10 007 with 64 / 96 / 192 MB 1 922 / 1 793 / 1 722 us.
@@ -285,7 +286,7 @@ CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   p.gt_floats = whole ? c * n4 : std::min(c128 * n4, std::max(kPieceFloats, 128 * n4));
   // at most 2 x SMs items of slices of dW^T (pick_slices)
   p.partial_floats = n > 0 ? std::min(2 * sms, std::max<int64_t>(div_up(n, BK), 1) * div_up(d, 128) * (c128 / 128)) * 128 * 128 : 0;
-  p.sums_floats = n > 0 ? kSplitGroups * std::max<int64_t>(2 * sms * 128, c128) : 0;  // a line per slice and group
+  p.sums_floats = n > 0 ? kSumLines * std::max<int64_t>(2 * sms * 128, c128) : 0;  // a line per slice and group
   p.slots = sms + div_up(n, BM);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += up256(bytes); return o; };
@@ -528,7 +529,7 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     const bool add = a.dw && slices > 1;
     if (add || a.db)
       GCNSA_STEP(launch_add_slices(s, add ? a.d : 0, width, slices, f_at(pl.partial), up4(width), add ? a.dw + c0 : nullptr, a.lddw, add ? dw_pad : width,
-                                   kSplitGroups * slices, f_at(pl.sums), a.db ? a.db + c0 : nullptr, a.accumulate));
+                                   kSumLines * slices, f_at(pl.sums), a.db ? a.db + c0 : nullptr, a.accumulate));
   }
   return 0;
 }

@@ -10,11 +10,11 @@
 // 1e-4 off.)
 //
 // One CTA per SM works on tiles of 128 x BN.  Warps 0 and 2 stream boxes of A and B into rings of shared memory with TMA.
-// Two groups of four warps (4-11) take every other k-block of A and leave it as three terms in tensor memory (a lane per row of
-// the tile, two k per 32-bit column), two more groups (12-19) every other k-block of B, as one or three terms in MN-major
-// tiles with the 128-byte swizzle.  (With both operands of a k-block in one group's hands, a stage that the MMAs had
-// given back stood empty for 1 700 clocks.)  Warp 1 issues the MMAs, and eight warps (20-27, two per lane quarter of tensor
-// memory, half the columns each) fold the accumulators and write the result: thread = row of the tile, so a result that is
+// Groups of four warps make the terms, a k-block of an operand each at a time: two for A (three where B is packed and its
+// terms are ready sooner), three terms in tensor memory (a lane per row of the tile, two k per 32-bit column), and two for B, one
+// or three terms in MN-major tiles with the 128-byte swizzle.  (With both operands of a k-block in one group's hands, a stage that the MMAs had
+// given back stood empty for 1 700 clocks.)  Warp 1 issues the MMAs, and eight warps (two per lane quarter of tensor memory,
+// half the columns each) fold the accumulators and write the result: thread = row of the tile, so a result that is
 // wanted transposed, D[m, n] at c[n * ldc + m], is written in lines of 128 bytes without a turn through shared memory.
 // Every product of this file is arranged so that this is the layout it needs.
 //
@@ -36,10 +36,7 @@ namespace gcnsa {
 namespace {
 
 constexpr int BM = 128, BK = 32;
-constexpr int kAWarp0 = 4, kBWarp0 = 12, kSplitGroups = 2, kFoldWarp0 = 20, kFoldWarps = 8, kTermThreads = 32 * (kFoldWarp0 + kFoldWarps);
-// registers per thread by role, in multiples of 8; their sum over the seven warpgroups is at most what the launch gives (72 each)
-constexpr int kRegsIssue = 32, kRegsA = 72, kRegsB = 64, kRegsFold = 96;
-static_assert(kRegsIssue + kSplitGroups * (kRegsA + kRegsB) + 2 * kRegsFold <= 7 * 72, "setmaxnreg draws on the registers of the launch");
+constexpr int kAWarp0 = 4, kFoldWarps = 8;
 constexpr int kSmallFolds = 8, kRetired = 8;
 constexpr int A_SLOT = BM * BK * 4;
 
@@ -56,7 +53,7 @@ struct Product {
   int64_t ldc, slice_stride;
   const int32_t* row_map;  // row(n), nullable; negative: not written
   int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros
-  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(kSplitGroups z + g) * sums_pitch + m]
+  float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(AG z + g) * sums_pitch + m]
   int64_t sums_pitch;
   int write;               // 0: only a_sums are wanted
   const float* a;          // ASrc::direct
@@ -181,6 +178,12 @@ struct TermShape {
   static constexpr bool P8 = P8_;
   static constexpr Out OUT = OUT_;
   static constexpr int NTB = P8 ? 1 : 3;                 // terms of B
+  static constexpr int AG = P8 ? 3 : 2, BG = 2;          // groups of four warps that make terms of A, of B
+  static constexpr int BWARP0 = kAWarp0 + 4 * AG, FWARP0 = BWARP0 + 4 * BG, THREADS = 32 * (FWARP0 + kFoldWarps);
+  // registers per thread by role, in multiples of 8; their sum over the warpgroups is at most what the launch gives
+  static constexpr int REGS = P8 ? 64 : 72;              // (the compiler's, with that many threads)
+  static constexpr int REGS_ISSUE = P8 ? 24 : 32, REGS_A = 72, REGS_B = P8 ? 48 : 64, REGS_FOLD = P8 ? 88 : 96;
+  static_assert(REGS_ISSUE + AG * REGS_A + BG * REGS_B + 2 * REGS_FOLD <= THREADS / 128 * REGS, "setmaxnreg draws on the registers of the launch");
   static constexpr int HALF = BN / 2;                    // columns of a fold warp
   // With one term of B all three products of a k-block share an accumulator, which is folded twice as often; the columns of
   // the third one hold more stages of A.
@@ -200,10 +203,10 @@ struct TermShape {
   // more than half of an SM's shared memory: a second CTA, which would wait for tensor memory, never shares the SM
   static constexpr int NEED = BAR_OFF + 512 + 1024;
   static constexpr int SMEM_BYTES = NEED > 118 * 1024 ? NEED : 118 * 1024;
-  static_assert(NA % kSplitGroups == 0 && NB % kSplitGroups == 0, "a slot belongs to one group");
-  // A group that waits for the MMAs of k-block g - NS has seen those of g - kSplitGroups - NS retire, so the phase before the
+  static_assert(NA % AG == 0 && NB % BG == 0, "a slot belongs to one group");
+  // A group that waits for the MMAs of k-block g - NS has seen those of g - NS - (its groups) retire, so the phase before the
   // last of that barrier, k-block g - NS - kRetired, has ended.
-  static_assert(kRetired >= kSplitGroups, "the phase before the last of a retire barrier has ended");
+  static_assert(kRetired >= AG && kRetired >= BG, "the phase before the last of a retire barrier has ended");
   static_assert(A_COL0 + NSA * A_COLS <= TMEM_COLS, "tensor memory has 512 columns");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
 };
@@ -241,53 +244,71 @@ __device__ __forceinline__ void term_items(int total, int& first, int& end, int&
 // the CTA whose run has item i
 __host__ __device__ inline int term_owner(int i, int total, int grid) { return (int)(((int64_t)(i + 1) * grid - 1) / total); }
 
-// A group's k-block of B: a lane has four neighbouring n of line(i), i below COUNT.  Loaded as a whole before the first term
-// is written: the compiler cannot tell that the boxes and the terms do not overlap, and line by line every load would wait for the
-// stores before it (1 370 clocks a k-block instead of 520).
-template <class S>
-struct TermB {
+// A group's k-block of B.  Loaded as a whole before the first term is written: the compiler cannot tell that the boxes and the terms
+// do not overlap, and line by line every load would wait for the stores before it.
+template <class S, bool P8 = S::P8>
+struct TermB {  // a lane has four neighbouring n of line(i), i below COUNT
   static constexpr int LANES = S::BN / 4, LINES = 32 / LANES, COUNT = 8 / LINES;  // lanes of a line, lines per instruction
-  float4 x[S::P8 ? 1 : COUNT];
-  uint32_t q[S::P8 ? COUNT : 1];
+  float4 x[COUNT];
   static __device__ __forceinline__ int line(int i, int wq, int lane) { return wq * 8 + i * LINES + lane / LANES; }
   __device__ __forceinline__ void load(const uint8_t* raw, int wq, int lane) {
     const int n = 4 * (lane % LANES);
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-      const int k = line(i, wq, lane);
-      if constexpr (S::P8) q[i] = *reinterpret_cast<const uint32_t*>(raw + k * S::BN + n);
-      else x[i] = *reinterpret_cast<const float4*>(raw + (n / 32) * 4096 + k * 128 + (n & 31) * 4);
-    }
+    for (int i = 0; i < COUNT; ++i) x[i] = *reinterpret_cast<const float4*>(raw + (n / 32) * 4096 + line(i, wq, lane) * 128 + (n & 31) * 4);
   }
-  // e8: the step of line wq * 8 + lane / (BN / 32), block lane % (BN / 32) of a packed B
-  __device__ __forceinline__ void store(uint8_t* terms, int wq, int lane, uint32_t e8) const {
+  __device__ __forceinline__ void store(uint8_t* terms, int wq, int lane, uint32_t) const {
     const int n = 4 * (lane % LANES);
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
       const int k = line(i, wq, lane);
       uint8_t* dst = terms + (n / 64) * 4096 + k * 128 + ((((n & 63) >> 3) ^ (k & 7)) << 4) + (n & 7) * 2;
-      if constexpr (S::P8) {
-        float v[4];
-        pack8_open(q[i], v);
-        constexpr int EB = S::BN / 32;
-        const float step = pack8_step(__shfl_sync(0xffffffffu, e8, (k & 7) * EB + n / 32));
-        const uint32_t a = __byte_perm(__float_as_uint(v[0] * step), __float_as_uint(v[1] * step), 0x7632);
-        const uint32_t b = __byte_perm(__float_as_uint(v[2] * step), __float_as_uint(v[3] * step), 0x7632);
-        *reinterpret_cast<uint2*>(dst) = make_uint2(a, b);
-      } else {
-        uint2 t0, t1, t2;
-        split3(x[i].x, x[i].y, t0.x, t1.x, t2.x);
-        split3(x[i].z, x[i].w, t0.y, t1.y, t2.y);
-        *reinterpret_cast<uint2*>(dst) = t0;
-        *reinterpret_cast<uint2*>(dst + S::B_TERM) = t1;
-        *reinterpret_cast<uint2*>(dst + 2 * S::B_TERM) = t2;
+      uint2 t0, t1, t2;
+      split3(x[i].x, x[i].y, t0.x, t1.x, t2.x);
+      split3(x[i].z, x[i].w, t0.y, t1.y, t2.y);
+      *reinterpret_cast<uint2*>(dst) = t0;
+      *reinterpret_cast<uint2*>(dst + S::B_TERM) = t1;
+      *reinterpret_cast<uint2*>(dst + 2 * S::B_TERM) = t2;
+    }
+  }
+};
+template <class S>
+struct TermB<S, true> {  // a lane has 16 neighbouring n, half a block of the checkpoint
+  static constexpr int LANES = S::BN / 16, LINES = 32 / LANES, COUNT = 8 / LINES;
+  uint4 q[COUNT];
+  static __device__ __forceinline__ int line(int i, int wq, int lane) { return wq * 8 + i * LINES + lane / LANES; }
+  __device__ __forceinline__ void load(const uint8_t* raw, int wq, int lane) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) q[i] = *reinterpret_cast<const uint4*>(raw + line(i, wq, lane) * S::BN + 16 * (lane % LANES));
+  }
+  // e8: the step of line wq * 8 + lane / (BN / 32), block lane % (BN / 32)
+  __device__ __forceinline__ void store(uint8_t* terms, int wq, int lane, uint32_t e8) const {
+    const int n = 16 * (lane % LANES);
+    const bool odd = n >= 64;  // the second block's lanes write their halves the other way round: all banks, once each
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      const int k = line(i, wq, lane);
+      const float step = pack8_step(__shfl_sync(0xffffffffu, e8, (k & 7) * (S::BN / 32) + n / 32));
+      uint8_t* dst = terms + (n / 64) * 4096 + k * 128;
+      const uint32_t half[2][2] = {{odd ? q[i].z : q[i].x, odd ? q[i].w : q[i].y}, {odd ? q[i].x : q[i].z, odd ? q[i].y : q[i].w}};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[4];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          float v[4];
+          pack8_open(half[h][p], v);
+          w[2 * p] = __byte_perm(__float_as_uint(v[0] * step), __float_as_uint(v[1] * step), 0x7632);
+          w[2 * p + 1] = __byte_perm(__float_as_uint(v[2] * step), __float_as_uint(v[3] * step), 0x7632);
+        }
+        const int chunk = ((n & 63) >> 3) + (h ^ (odd ? 1 : 0));
+        *reinterpret_cast<uint4*>(dst + ((chunk ^ (k & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
 };
 
 template <class S>
-__global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_constant__ TermArgs args) {
+__global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_constant__ TermArgs args) {
   constexpr int BN = S::BN, NA = S::NA, NB = S::NB, NSA = S::NSA, NSB = S::NSB, NTB = S::NTB, HALF = S::HALF;
   constexpr bool A_TMA = S::A != ASrc::direct;
   extern __shared__ uint8_t smem_raw[];
@@ -355,7 +376,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
   term_items<S>(args.total, w0, w_end, w_step);
 
   if (warp < kAWarp0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::REGS_ISSUE));
     if ((warp == 0 && A_TMA) || warp == 2) {
       // ---------------- TMA producers: warp 0 streams A, warp 2 streams B ----------------
       if (elect_one()) {
@@ -461,9 +482,10 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         }
       }
     }
-  } else if (warp < kBWarp0) {
-    // ---------------- terms of A (warps 4..11): every other k-block to a group ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsA));
+  } else if (warp < S::BWARP0) {
+    // ---------------- terms of A: every AG-th k-block to a group ----------------
+    if constexpr (S::REGS_A > S::REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::REGS_A));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::REGS_A));
     const int q = warp & 3, group = (warp - kAWarp0) >> 2, row = 32 * q + lane;  // row of the tile
     uint32_t g = 0;
     bool ok = true;
@@ -476,9 +498,9 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       const float* const a_at = A_TMA ? nullptr : p.a + wk.m0 + row;
       const int64_t lda = p.lda, k_rows = p.k_rows;
       const bool in_m = wk.m0 + row < p.M;
-      int it = (int)((g + group) % kSplitGroups);  // first k-block of this group in the item
+      int it = (int)((group + S::AG - g % S::AG) % S::AG);  // first k-block of this group in the item
       g += it;
-      for (; it < wk.n_kb; it += kSplitGroups, g += kSplitGroups) {
+      for (; it < wk.n_kb; it += S::AG, g += S::AG) {
         float x[32];
         if constexpr (!A_TMA) {
           const int64_t k0 = (int64_t)(wk.kb0 + it) * BK;
@@ -533,33 +555,34 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       }
       if (!ok) break;
       g -= it - wk.n_kb;  // k-blocks of all groups
-      if (sums && in_m) p.a_sums[(kSplitGroups * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
+      if (sums && in_m) p.a_sums[(S::AG * (int64_t)wk.z + group) * p.sums_pitch + wk.m0 + row] = a_sum;
     }
-  } else if (warp < kFoldWarp0) {
-    // ---------------- terms of B (warps 12..19) ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsB));
-    const int q = warp & 3, group = (warp - kBWarp0) >> 2;
+  } else if (warp < S::FWARP0) {
+    // ---------------- terms of B ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::REGS_B));
+    const int q = warp & 3, group = (warp - S::BWARP0) >> 2;
     uint32_t g = 0;
     bool ok = true;
     for (int w = w0; ok && w < w_end; w += w_step) {
       const TermWork wk = term_work(args, w, BN);
       const Product& p = args.p[wk.prob];
       // steps of a packed B: a lane has the one of line q * 8 + lane / (BN / 32) of the k-block, block lane % (BN / 32) of the
-      // tile; fetched one k-block (of this group) ahead
-      uint32_t e_next = 0;
+      // tile; fetched three k-blocks (of this group) ahead
       constexpr int EB = BN / 32;
       const int64_t lde = p.lde, k_left = p.k_rows - ((int64_t)wk.kb0 * BK + q * 8 + lane / EB);
       const uint8_t* const e_at = p.e + (p.k_rows - k_left) * lde + wk.n0 / 32 + lane % EB;
       const bool e_in = S::P8 && lane < 8 * EB && wk.n0 / 32 + lane % EB < p.e_blocks;
-      auto fetch_e = [&](int it) {
-        if constexpr (S::P8) e_next = e_in && it < wk.n_kb && it * BK < k_left ? __ldg(e_at + (int64_t)it * BK * lde) : 0u;
-      };
-      int it = (int)((g + group) % kSplitGroups);
+      auto step_of = [&](int it) { return e_in && it < wk.n_kb && it * BK < k_left ? __ldg(e_at + (int64_t)it * BK * lde) : 0u; };
+      int it = (int)((group + S::BG - g % S::BG) % S::BG);
       g += it;
-      fetch_e(it);
-      for (; it < wk.n_kb; it += kSplitGroups, g += kSplitGroups) {
-        const uint32_t sb = g % NSB, e8 = e_next;
-        fetch_e(it + kSplitGroups);
+      uint32_t e_next[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) e_next[i] = step_of(it + i * S::BG);
+      for (; it < wk.n_kb; it += S::BG, g += S::BG) {
+        const uint32_t sb = g % NSB, e8 = e_next[0];
+        e_next[0] = e_next[1];
+        e_next[1] = e_next[2];
+        e_next[2] = step_of(it + 3 * S::BG);
         ok = __all_sync(0xffffffffu, mbar_wait_long(&full_b[g % NB], (g / NB) & 1, 44));
         if (!ok) break;
         TermB<S> tb;
@@ -578,9 +601,9 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
       g -= it - wk.n_kb;
     }
   } else {
-    // ---------------- folds and results (warps 20..27) ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsFold));
-    const int quad = warp & 3, half = (warp - kFoldWarp0) >> 2;
+    // ---------------- folds and results ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::REGS_FOLD));
+    const int quad = warp & 3, half = (warp - S::FWARP0) >> 2;
     const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + half * HALF;
     uint32_t folds = 0;
     float run_m = -INFINITY, run_s = 0.f;  // (Out::stats)
@@ -676,7 +699,7 @@ __global__ void __launch_bounds__(kTermThreads, 1) term_product(const __grid_con
         const int cols = min(HALF, p.N - nb);  // classes of this half (may be below 1)
         const int c0 = args.ce.c0 + nb;
         if (args.ce.bias) {
-          float* const xb = reinterpret_cast<float*>(smem + S::X_OFF) + (warp - kFoldWarp0) * HALF;
+          float* const xb = reinterpret_cast<float*>(smem + S::X_OFF) + (warp - S::FWARP0) * HALF;
 #pragma unroll
           for (int j = 0; j < HALF; j += 32) xb[j + lane] = j + lane < cols ? __ldg(args.ce.bias + c0 + j + lane) : 0.f;
           __syncwarp();
@@ -797,7 +820,7 @@ template <class S>
 cudaError_t run_terms(cudaStream_t s, const TermArgs& a, int grid) {
   cudaError_t e = cudaFuncSetAttribute(term_product<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  return launch(term_product<S>, grid, kTermThreads, S::SMEM_BYTES, s, a);
+  return launch(term_product<S>, grid, S::THREADS, S::SMEM_BYTES, s, a);
 }
 
 }  // namespace
