@@ -1703,6 +1703,8 @@ int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const floa
                        int64_t lddh, float* dw, int64_t lddw, float* db, int32_t accumulate, void* workspace,
                        size_t workspace_bytes) {
   if (n < 0 || d < 1 || c < 1 || n_train < 0 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension, d < 1 or c < 1");
+  // tiles of 128 x 128 logits are counted in 32 bits
+  if (((n + 127) / 128) * (((int64_t)c + 127) / 128) >= INT32_MAX) return fail(GCNSA_ERR_TOO_LARGE, "n c / 16384 exceeds int32 indexing");
   if (n_train > n || (!mask && n_train != n)) return fail(GCNSA_ERR_ARG, "n_train is the number of masked rows");
   if (!loss || !w || (n > 0 && (!h || !y))) return fail(GCNSA_ERR_ARG, "NULL pointer");
   if (ldw < c || (dw && lddw < c) || (n > 0 && (ldh < d || (dh && lddh < d)))) return fail(GCNSA_ERR_ARG, "leading dimension too small");

@@ -151,89 +151,96 @@ gather_rows(int64_t n, int d, const float* __restrict__ h, int64_t ldh, const in
   }
 }
 
-// logsumexp of every row from the runs that crossed its tile, and its loss
-__global__ void __launch_bounds__(256)
-row_finish(int64_t rows, int tiles_n, int total, int grid, const float* __restrict__ part_m, const float* __restrict__ part_s,
-           const float* __restrict__ zy, float* __restrict__ lse, float* __restrict__ row_loss) {
-  wait_for_predecessors();
-  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (r >= rows) return;
-  const int t = (int)(r / BM);
-  const int b0 = term_owner(t * tiles_n, total, grid), b1 = term_owner((t + 1) * tiles_n - 1, total, grid);
-  float m = -INFINITY, s = 0.f;
-  for (int b = b0; b <= b1; ++b)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t slot = ((int64_t)(b + t) * 2 + h) * BM + r % BM;
-      const float pm = part_m[slot], top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
-      s = s * expf(m - base) + part_s[slot] * expf(pm - base);
-      m = top;
-    }
-  const float l = (m == -INFINITY ? 0.f : m) + logf(s);
-  lse[r] = l;
-  row_loss[r] = l - zy[r];
-}
-// Sums of row losses and the number of rows that count, a partial of both per block; the block that is alone finishes.
-struct LossSum {
-  double loss;
-  long long count;
-};
-__device__ __forceinline__ void finish_loss(const LossSum& s, long long count, int64_t n_train, float* loss) {
-  *loss = count != n_train ? NAN : n_train > 0 ? (float)(s.loss / (double)n_train) : 0.f;
-}
-constexpr int kLossThreads = 512, kLossBlocks = 148;
-// mask (with rows that are not gathered): counted here; total: counted before; neither: all rows count
-__global__ void __launch_bounds__(kLossThreads)
-loss_sums(int64_t rows, const float* __restrict__ row_loss, const uint8_t* __restrict__ mask, const int* __restrict__ total,
-          int64_t n_train, LossSum* __restrict__ partial, float* __restrict__ loss) {
-  wait_for_predecessors();
-  __shared__ double shl[kLossThreads / 32];
-  __shared__ int shc[kLossThreads / 32];
-  double s = 0.0;
-  int count = 0;
+// The loss from the sums of warps or blocks, in a fixed order: 256 threads.
+__device__ __forceinline__ void finish_loss(int n, const LossSum* __restrict__ sums, const int* __restrict__ total, int64_t n_train, float* __restrict__ loss) {
+  __shared__ double shl[8];
+  __shared__ long long shc[8];
+  LossSum a = {0.0, 0};
 #pragma unroll 4
-  for (int64_t r = (int64_t)blockIdx.x * kLossThreads + threadIdx.x; r < rows; r += (int64_t)gridDim.x * kLossThreads) {
-    s += row_loss[r];
-    count += !mask || mask[r] != 0;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    a.loss += sums[i].loss;
+    a.count += sums[i].count;
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-  count = __reduce_add_sync(kFull, count);
+  for (int o = 16; o > 0; o >>= 1) {
+    a.loss += __shfl_xor_sync(kFull, a.loss, o);
+    a.count += __shfl_xor_sync(kFull, a.count, o);
+  }
   if ((threadIdx.x & 31) == 0) {
-    shl[threadIdx.x >> 5] = s;
-    shc[threadIdx.x >> 5] = count;
+    shl[threadIdx.x >> 5] = a.loss;
+    shc[threadIdx.x >> 5] = a.count;
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
-  LossSum a = {0.0, 0};
-  for (int w = 0; w < kLossThreads / 32; ++w) {
+  for (int w = 1; w < 8; ++w) {
     a.loss += shl[w];
     a.count += shc[w];
   }
-  if (gridDim.x == 1) finish_loss(a, total ? *total : a.count, n_train, loss);
-  else partial[blockIdx.x] = a;
+  const long long count = total ? *total : a.count;
+  *loss = count != n_train ? NAN : n_train > 0 ? (float)(a.loss / (double)n_train) : 0.f;
 }
-__global__ void __launch_bounds__(32)
-loss_total(int blocks, const LossSum* __restrict__ partial, const int* __restrict__ total, int64_t n_train, float* __restrict__ loss) {
+__global__ void __launch_bounds__(256) loss_total(int n, const LossSum* __restrict__ sums, const int* __restrict__ total, int64_t n_train, float* __restrict__ loss) {
   wait_for_predecessors();
-  if (threadIdx.x != 0) return;
-  LossSum a = {0.0, 0};
-  for (int b = 0; b < blocks; ++b) {
-    a.loss += partial[b].loss;
-    a.count += partial[b].count;
-  }
-  finish_loss(a, total ? *total : a.count, n_train, loss);
+  finish_loss(n, sums, total, n_train, loss);
 }
+// logsumexp of every row from the runs that crossed its tile, and a block's sum of losses
+__global__ void __launch_bounds__(256)
+row_finish(int64_t rows, int c, int tiles_n, int total, int grid, const float* __restrict__ part_m, const float* __restrict__ part_s,
+           const int32_t* __restrict__ y, const float* __restrict__ zy, float* __restrict__ lse, LossSum* __restrict__ losses) {
+  wait_for_predecessors();
+  __shared__ double sh[8];
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  double loss = 0.0;
+  if (r < rows) {
+    const int t = (int)(r / BM);
+    const int b0 = term_owner(t * tiles_n, total, grid), b1 = term_owner((t + 1) * tiles_n - 1, total, grid);
+    float m = -INFINITY, s = 0.f;
+    for (int b = b0; b <= b1; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t slot = ((int64_t)(b + t) * 2 + h) * BM + r % BM;
+        const float pm = part_m[slot], top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
+        s = s * expf(m - base) + part_s[slot] * expf(pm - base);
+        m = top;
+      }
+    const float l = (m == -INFINITY ? 0.f : m) + logf(s);
+    const int label = y[r];
+    lse[r] = l;
+    loss = label >= 0 && label < c ? l - zy[r] : NAN;  // (no class was a label outside)
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(kFull, loss, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = loss;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) loss += sh[w];
+    losses[blockIdx.x] = LossSum{loss, (long long)min((int64_t)256, rows - (int64_t)blockIdx.x * 256)};
+  }
+}
+// what finish_loss is given
+struct LossEnd {
+  int n = 0;
+  const LossSum* sums = nullptr;
+  const int* total = nullptr;
+  int64_t n_train = 0;
+  float* loss = nullptr;  // NULL: not to be written
+};
 // The slices of a product added up, and with them the sums that its left operand left: row r of c (+)= sum over the slices of
-// partial[z][r][.] for r < rows, and sums_out (+)= sum over `lines` lines of sums.  A block has 128 columns of a row; its 8 warps
+// partial[z][r][.] for r < rows, and sums_out (+)= sum over `lines` lines of sums; with them the loss, where it is still to be
+// made.  A block has 128 columns of a row; its 8 warps
 // take every 8th slice each, a float4 to a lane, and are added in warp order.
 __global__ void __launch_bounds__(256)
 add_slices(int rows, int n, int slices, const float* __restrict__ partial, int64_t ldp, float* __restrict__ c, int64_t ldc, int n_pad, int lines,
-           const float* __restrict__ sums, float* __restrict__ sums_out, int accumulate) {
+           const float* __restrict__ sums, float* __restrict__ sums_out, int accumulate, LossEnd end) {
   wait_for_predecessors();
+  if (end.loss && blockIdx.y == gridDim.y - 1) {  // a line of blocks of its own
+    if (blockIdx.x == 0) finish_loss(end.n, end.sums, end.total, end.n_train, end.loss);
+    return;
+  }
+  const int lines_y = gridDim.y - (end.loss != nullptr);
   __shared__ float4 sh[8][32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, j = 128 * blockIdx.x + 4 * lane;
-  for (int r = blockIdx.y; r < rows + (sums_out != nullptr); r += gridDim.y) {
+  for (int r = blockIdx.y; r < rows + (sums_out != nullptr); r += lines_y) {
     const bool tail = r == rows;
     const float* src = tail ? sums + j : partial + r * ldp + j;
     const int64_t step = tail ? ldp : rows * ldp;
@@ -262,9 +269,9 @@ add_slices(int rows, int n, int slices, const float* __restrict__ partial, int64
 }
 // (pitch of both partial and sums: ldp)
 int launch_add_slices(cudaStream_t s, int64_t rows, int64_t n, int slices, const float* partial, int64_t ldp, float* c, int64_t ldc, int64_t n_pad,
-                      int lines, const float* sums, float* sums_out, int accumulate) {
-  const dim3 grid((unsigned)((n_pad + 127) / 128), (unsigned)std::min<int64_t>(rows + (sums_out != nullptr), 65535));
-  const cudaError_t e = launch(add_slices, grid, 256, 0, s, rows, n, slices, partial, ldp, c, ldc, n_pad, lines, sums, sums_out, accumulate);
+                      int lines, const float* sums, float* sums_out, int accumulate, const LossEnd& end = LossEnd{}) {
+  const dim3 grid((unsigned)((n_pad + 127) / 128), (unsigned)std::min<int64_t>(rows + (sums_out != nullptr), 65000) + (end.loss != nullptr));
+  const cudaError_t e = launch(add_slices, grid, 256, 0, s, rows, n, slices, partial, ldp, c, ldc, n_pad, lines, sums, sums_out, accumulate, end);
   note_launch();
   return (int)e;
 }
@@ -277,7 +284,7 @@ constexpr int kWholeCols = 128;                    // classes that one tile hold
 constexpr int64_t kPieceFloats = int64_t(40) << 20;
 struct CePlan {
   int64_t gt_floats, partial_floats, sums_floats, slots;
-  size_t gt, partial, sums, hc, wc, yc, rows, place, counts, total, zy, lse, row_loss, part, losses, end;
+  size_t gt, partial, sums, hc, wc, yc, rows, place, counts, total, zy, lse, part, losses, end;
 };
 CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   CePlan p;
@@ -302,9 +309,8 @@ CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   p.total = take(4);
   p.zy = take((size_t)n * 4);
   p.lse = take((size_t)n * 4);
-  p.row_loss = take((size_t)n * 4);
   p.part = take((size_t)p.slots * 2 * BM * 2 * 4);
-  p.losses = take(kLossBlocks * sizeof(LossSum));
+  p.losses = take((size_t)std::max<int64_t>(sms * kFoldWarps, div_up(n, 256)) * sizeof(LossSum));
   p.end = at;
   return p;
 }
@@ -429,19 +435,25 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     p.units = (int)div_up(a.d, BK);
     p.k_rows = a.d;
   }
-  // loss
+  // loss: sums of warps or blocks, which the first launch of add_slices finishes
+  LossSum* const losses = (LossSum*)(ws + pl.losses);
+  LossEnd end;
+  end.sums = losses;
+  end.total = total;
+  end.n_train = a.n_train;
+  end.loss = a.loss;
   if (R > 0 && whole) {
     t.ce.mask = a.mask;
     t.ce.gt = grads ? f_at(pl.gt) : nullptr;
-    t.ce.row_loss = f_at(pl.row_loss);
+    t.ce.losses = losses;
     set_slices(t.p[0], a.c <= 64 ? 64 : 128, 1);
     t.total = t.p[0].items;
     const int grid = std::min(t.total, sms);
+    end.n = grid * kFoldWarps;
     GCNSA_STEP(a.c <= 64 ? run_terms<TermShape<64, ASrc::kMajor, false, Out::whole>>(s, t, grid)
                          : run_terms<TermShape<128, ASrc::kMajor, false, Out::whole>>(s, t, grid));
     note_launch();
   } else if (R > 0) {
-    GCNSA_STEP(cudaMemsetAsync(ws + pl.zy, 0xff, (size_t)R * 4, s));  // NaN: no class was the row's label
     t.ce.zy = f_at(pl.zy);
     t.ce.part_m = f_at(pl.part);
     t.ce.part_s = f_at(pl.part) + pl.slots * 2 * BM;
@@ -449,17 +461,16 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     t.total = t.p[0].items;
     const int grid = std::min(t.total, sms);
     GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::stats>>(s, t, grid)));
-    GCNSA_STEP(launch(row_finish, (int)div_up(R, 256), 256, 0, s, R, t.p[0].tiles_n, t.total, grid, (const float*)t.ce.part_m, (const float*)t.ce.part_s,
-                      (const float*)t.ce.zy, f_at(pl.lse), f_at(pl.row_loss)));
+    end.n = (int)div_up(R, 256);
+    GCNSA_STEP(launch(row_finish, end.n, 256, 0, s, R, a.c, t.p[0].tiles_n, t.total, grid, (const float*)t.ce.part_m, (const float*)t.ce.part_s,
+                      y, (const float*)t.ce.zy, f_at(pl.lse), losses));
     note_launch(2);
     t.ce.lse = f_at(pl.lse);
   }
-  {
-    const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(div_up(R, 16 * kLossThreads), kLossBlocks));
-    GCNSA_STEP(launch(loss_sums, blocks, kLossThreads, 0, s, R, (const float*)f_at(pl.row_loss), whole ? a.mask : nullptr, total, a.n_train,
-                      (LossSum*)(ws + pl.losses), a.loss));
-    if (blocks > 1) GCNSA_STEP(launch(loss_total, 1, 32, 0, s, blocks, (const LossSum*)(ws + pl.losses), total, a.n_train, a.loss));
-    note_launch(blocks > 1 ? 2 : 1);
+  if (!grads || R == 0 || (!a.dw && !a.db)) {  // no launch of add_slices to come
+    GCNSA_STEP(launch(loss_total, 1, 256, 0, s, end.n, (const LossSum*)losses, total, a.n_train, a.loss));
+    note_launch();
+    end.loss = nullptr;
   }
   if (!grads) return 0;
   if (R == 0) {  // nothing counts: sums of nothing
@@ -527,9 +538,11 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::transposed>>(s, b, std::min(b.total, sms))));
     note_launch();
     const bool add = a.dw && slices > 1;
-    if (add || a.db)
+    if (add || a.db || end.loss) {
       GCNSA_STEP(launch_add_slices(s, add ? a.d : 0, width, slices, f_at(pl.partial), up4(width), add ? a.dw + c0 : nullptr, a.lddw, add ? dw_pad : width,
-                                   kSumLines * slices, f_at(pl.sums), a.db ? a.db + c0 : nullptr, a.accumulate));
+                                   kSumLines * slices, f_at(pl.sums), a.db ? a.db + c0 : nullptr, a.accumulate, end));
+      end.loss = nullptr;
+    }
   }
   return 0;
 }

@@ -33,10 +33,14 @@ __device__ __forceinline__ void load_row(const float* row, int f, int t, float (
     if constexpr (VEC) {
       const int c = 4 * (v * T + t);
       const float4 a = c < f ? *reinterpret_cast<const float4*>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-      x[4 * v] = a.x;  // (c < f)
-      x[4 * v + 1] = c + 1 < f ? a.y : 0.f;
-      x[4 * v + 2] = c + 2 < f ? a.z : 0.f;
-      x[4 * v + 3] = c + 3 < f ? a.w : 0.f;
+      x[4 * v] = a.x;
+      x[4 * v + 1] = a.y;
+      x[4 * v + 2] = a.z;
+      x[4 * v + 3] = a.w;
+      if (f & 3) {  // pad columns may hold anything
+#pragma unroll
+        for (int k = 1; k < 4; ++k) x[4 * v + k] = c + k < f ? x[4 * v + k] : 0.f;
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -53,9 +57,13 @@ __device__ __forceinline__ void store_row(float* row, int f, int n_pad, int t, c
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {
       const int c = 4 * (v * T + t);
-      if (c < f)
-        *reinterpret_cast<float4*>(row + c) = make_float4(x[4 * v], c + 1 < f ? x[4 * v + 1] : 0.f, c + 2 < f ? x[4 * v + 2] : 0.f,
-                                                          c + 3 < f ? x[4 * v + 3] : 0.f);
+      float4 a = make_float4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
+      if (f & 3) {
+        a.y = c + 1 < f ? a.y : 0.f;
+        a.z = c + 2 < f ? a.z : 0.f;
+        a.w = c + 3 < f ? a.w : 0.f;
+      }
+      if (c < f) *reinterpret_cast<float4*>(row + c) = a;
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -83,9 +91,9 @@ __device__ __forceinline__ void load_packed(const PackedRows& p, int64_t row, in
       const uint32_t q4 = c < f ? *reinterpret_cast<const uint32_t*>(q + c) : 0u;
       const float step = c < f ? pack8_step(e[c / kPackBlock]) : 0.f;
       float a[4];
-      pack8_open(q4, a);
+      pack8_open(q4, a);  // (pad bytes are zeros)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[4 * v + k] = c + k < f ? a[k] * step : 0.f;
+      for (int k = 0; k < 4; ++k) x[4 * v + k] = a[k] * step;
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -670,7 +678,12 @@ int norm_blocks(int64_t n, int teams, int most) { return (int)std::max<int64_t>(
 int grad_teams(int32_t f) { return f <= kNarrowCols ? kNormThreads : f <= 32 ? 32 : f <= 64 ? 16 : f <= 512 ? 8 : 1; }
 // (float4 of a row to a thread, as launch_layer_norm_grad has it)
 int grad_nv(int32_t f) { return f <= 128 ? 1 : f <= 256 ? 2 : f <= 512 ? 4 : f <= 1024 ? 1 : f <= 2048 ? 2 : f <= 4096 ? 4 : 8; }
-int grad_blocks(int64_t n, int32_t f) { return norm_blocks(n, grad_teams(f), 148 * (f > kNormMaxCols ? 4 : grad_blocks_per_sm(grad_nv(f)))); }
+int grad_blocks(int64_t n, int32_t f) {
+  // rows too wide for registers: a block's partial sums are as wide, and all of them take at most 256 MB
+  const int64_t most = f > kNormMaxCols ? std::max<int64_t>(1, std::min<int64_t>(148 * 4, (int64_t(256) << 20) / (8 * (int64_t)f)))
+                                        : 148 * grad_blocks_per_sm(grad_nv(f));
+  return norm_blocks(n, grad_teams(f), (int)most);
+}
 
 }  // namespace
 

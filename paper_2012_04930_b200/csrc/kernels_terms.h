@@ -62,6 +62,11 @@ struct Product {
   int64_t lde;
   int e_blocks;
 };
+// Sum of row losses and number of rows that count.
+struct LossSum {
+  double loss;
+  long long count;
+};
 // The epilogues of the output layer; D[m, n] is a logit without its bias, m a row, n a class of the piece from c0 on.
 struct CeTile {
   const float* bias;     // nullable, of the whole layer
@@ -72,7 +77,7 @@ struct CeTile {
   float* gt;             // G^T: [class of the piece][ldg]; nullable (Out::whole)
   const float* lse;      // [M] (Out::grad)
   float *part_m, *part_s, *zy;  // (Out::stats) running maximum and sum of a CTA's run in a row tile, the label's logit
-  float* row_loss;       // [M] (Out::whole)
+  LossSum* losses;       // (Out::whole) a sum per fold warp of the grid
 };
 struct TermArgs {
   Product p[2];
@@ -608,6 +613,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
     uint32_t folds = 0;
     float run_m = -INFINITY, run_s = 0.f;  // (Out::stats)
     uint32_t met = 0;                      // (Out::whole) meetings of the two warps of a quarter
+    LossSum mine = {0.0, 0};
     bool ok = true;
     auto meet = [&]() {  // what either wrote to shared memory before is there for the other one; false: a wait ran out
       __syncwarp();
@@ -649,16 +655,16 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
             for (int j = 0; j < 16; ++j) sum[c0 + j] += __uint_as_float(v[j]);
           }
         };
-        fold(lanes + (folds & 1) * BN);
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&acc_empty[folds & 1]);
-        if (small) {
+        if (small) {  // first: the MMAs of the next item wait for it, while they have another accumulator for the leading terms
           fold(lanes + 2 * BN);
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(small_empty);
         }
+        fold(lanes + (folds & 1) * BN);
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&acc_empty[folds & 1]);
       }
       if (!ok) break;
       if constexpr (S::OUT == Out::transposed) {
@@ -778,8 +784,12 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
             s = xs[r] + xs[BM + r];
             if (row_in) {
               const float inv = 1.f / s;
-              if (here || (half == 0 && (label + c0 < 0 || label + c0 >= p.N)))  // (a label outside: no logit)
-                args.ce.row_loss[m] = !on ? 0.f : here ? (base + logf(s)) - zy : NAN;
+              // the half that has the label's logit adds the row's loss (a label outside all classes: no loss is a number)
+              if (on && here) mine.loss += (base + logf(s)) - zy;
+              if (on && half == 0) {
+                if (label + c0 < 0 || label + c0 >= p.N) mine.loss = NAN;
+                ++mine.count;
+              }
               if (args.ce.gt) {
                 const int64_t ldg = args.ce.ldg;
                 float* at = args.ce.gt + nb * ldg + m;
@@ -791,6 +801,14 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
           }
         }
       }
+    }
+    if constexpr (S::OUT == Out::whole) {  // (a fixed order; written also where a wait ran out, as all of them are read)
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        mine.loss += __shfl_xor_sync(0xffffffffu, mine.loss, o);
+        mine.count += __shfl_xor_sync(0xffffffffu, mine.count, o);
+      }
+      if (lane == 0) args.ce.losses[blockIdx.x * kFoldWarps + warp - S::FWARP0] = mine;
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

@@ -469,6 +469,31 @@ def test_output_layer_extreme_logits(c):
     assert torch.isfinite(got["dh"][:7]).all() and torch.isfinite(got["dh"][8:]).all()
 
 
+@pytest.mark.parametrize("n,d,c", [(5000, 256, 1000), (9000, 128, 41), (2500, 602, 300)])
+def test_output_layer_has_the_same_bits_from_run_to_run(n, d, c):
+    """The pipelines of the products keep their order whatever lands first: loss and gradients of 40 calls, others between them."""
+    h, w, bias = torch.relu(_rand(n, n, d)) * 2, _rand(d, d, c) / math.sqrt(d), _rand(c, c)
+    y = torch.arange(n, device="cuda", dtype=torch.int32) % c
+    mask = (_rand(3, n) < 0.5).to(torch.uint8)
+    first = _ce_run(h, w, bias, y, mask, int(mask.sum()))
+    for i in range(40):
+        if i % 4 == 0:
+            _ce_run(h[:777], w, None, y[:777], None, 777)
+        again = _ce_run(h, w, bias, y, mask, int(mask.sum()))
+        assert all(torch.equal(first[k], again[k]) for k in first), i
+
+
+@pytest.mark.parametrize("n,f,c,padded", [(60_000, 256, 256, True), (20_000, 500, 64, True), (30_000, 64, 130, False)])
+def test_weight_gradient_has_the_same_bits_from_run_to_run(n, f, c, padded):
+    p, g = gcnsa.Packed8(n, f), _buf(_rand(1, n, c), padded)
+    gcnsa.op_pack8(_rand(2, n, f), p)
+    ws, first, again = _bytes(gcnsa.op_gemm_packed8_workspace(n, f, c)), torch.empty(f, c, device="cuda"), torch.empty(f, c, device="cuda")
+    gcnsa.op_gemm_packed8(p, g, c, first, workspace=ws)
+    for _ in range(60):
+        gcnsa.op_gemm_packed8(p, g, c, again, workspace=ws)
+        assert torch.equal(first, again)
+
+
 # ---------------------------------------------------------- all together ---
 def _step(x, rp, cc, vv, w, gamma, beta, wo, bo, y, mask, nt, out):
     """One training step of  H = relu(norm(A (X W)));  z = H Wo + bo, its hidden rows kept as checkpoints only."""

@@ -56,6 +56,7 @@ def test_layer_norm_refusals():
     assert bwd(ldg=100) == gcnsa.ERR_ARG and bwd(ldx=100) == gcnsa.ERR_ARG and bwd(lddx=100) == gcnsa.ERR_ARG
     assert bwd(dx=BASE, lddx=256) == gcnsa.ERR_ARG and bwd(dx=BASE + 0x100000, lddx=256) == gcnsa.ERR_ARG
     need = gcnsa.op_layer_norm_backward_scratch(100, 128)
+    assert gcnsa.op_layer_norm_backward_scratch(10**6, 1 << 24) <= 1 << 29     # partial sums of wide rows are bounded
     assert need >= 2 * 128 * 4 and bwd(sbytes=need - 1) == gcnsa.ERR_ARG and bwd(scratch=BASE + 2) == gcnsa.ERR_ARG
 
 
@@ -92,6 +93,7 @@ def test_output_layer_refusals():
     assert ce(n=-1) == gcnsa.ERR_ARG and ce(d=0) == gcnsa.ERR_ARG and ce(c=0) == gcnsa.ERR_ARG and ce(n=2**31 - 1) == gcnsa.ERR_ARG
     for k in ("h", "w", "y", "loss", "ws"):
         assert ce(**{k: None}) == gcnsa.ERR_ARG, k
+    assert ce(n=2**31 - 2, c=2**31 - 1, n_train=5, ldw=2**31, lddw=2**31) == gcnsa.ERR_TOO_LARGE
     assert ce(ldh=63) == gcnsa.ERR_ARG and ce(ldw=499) == gcnsa.ERR_ARG and ce(lddh=63) == gcnsa.ERR_ARG and ce(lddw=499) == gcnsa.ERR_ARG
     assert ce(n_train=-1) == gcnsa.ERR_ARG and ce(n_train=1001) == gcnsa.ERR_ARG
     assert ce(mask=None, n_train=999) == gcnsa.ERR_ARG                 # without a mask every row counts
