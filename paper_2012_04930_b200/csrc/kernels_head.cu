@@ -247,7 +247,7 @@ add_slices(int rows, int n, int slices, const float* __restrict__ partial, int64
     const int count = tail ? lines : slices;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j < n) {
-#pragma unroll 4
+#pragma unroll 8
       for (int z = w; z < count; z += 8) {
         const float4 v = __ldg(reinterpret_cast<const float4*>(src + z * step));
         a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;

@@ -37,10 +37,6 @@ __device__ __forceinline__ void load_row(const float* row, int f, int t, float (
       x[4 * v + 1] = a.y;
       x[4 * v + 2] = a.z;
       x[4 * v + 3] = a.w;
-      if (f & 3) {  // pad columns may hold anything
-#pragma unroll
-        for (int k = 1; k < 4; ++k) x[4 * v + k] = c + k < f ? x[4 * v + k] : 0.f;
-      }
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -49,6 +45,13 @@ __device__ __forceinline__ void load_row(const float* row, int f, int t, float (
       }
     }
   }
+}
+// ... and, when all loads of a row are under way, zeros for the pad columns in it, which may hold anything
+template <int T, int NV, bool VEC>
+__device__ __forceinline__ void clear_pads(int f, int t, float (&x)[4 * NV]) {
+  if (VEC && (f & 3))
+#pragma unroll
+    for (int i = 0; i < 4 * NV; ++i) x[i] = col_of<T, VEC>(i / 4, i % 4, t) < f ? x[i] : 0.f;
 }
 // the row's pad columns up to the next multiple of 4 come out as zeros (n_pad)
 template <int T, int NV, bool VEC>
@@ -229,6 +232,7 @@ layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __re
     const bool in = row < n;
     float a[4 * NV];
     load_row<T, NV, VEC>(x + row * ldx, in ? f : 0, t, a);
+    clear_pads<T, NV, VEC>(f, t, a);
     if (x8.q) store_packed<T, NV, VEC>(x8, row, in, f, t, a);
     float s[1] = {0.f};
 #pragma unroll
@@ -309,6 +313,8 @@ layer_norm_grad(int64_t n, int f, const float* g, int64_t ldg, const float* x, i
     else load_row<T, NV, VEC>(x + row * ldx, in ? f : 0, t, a);
     load_row<T, NV, VEC>(g + row * ldg, in ? f : 0, t, u);
     const float mu = in ? mean[row] : 0.f, r = in ? rstd[row] : 0.f;
+    if constexpr (!X8) clear_pads<T, NV, VEC>(f, t, a);
+    clear_pads<T, NV, VEC>(f, t, u);
     if (relu) {
       if (bits.w) {
 #pragma unroll
