@@ -2,7 +2,7 @@
 //
 // All of these read and write whole matrices once and compute little, so memory bounds them: a row is loaded once, stays in
 // registers through its sums, and is written once.  A row belongs to a team of T threads (8, 16 or 32 lanes, or a block of
-// 256) that holds NV float4 of it each; a warp works on 32 / T rows at a time.
+// 256) that holds NV float4 of it each; a warp works on 32 / T rows at a time, times R where rows are short.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -20,7 +20,7 @@ constexpr int kNormThreads = 256;
 constexpr int kNormMaxCols = 8192;  // columns that 256 threads hold in registers
 
 // Column k of chunk v of thread t: four neighbours to a thread where rows take 16-byte accesses, neighbouring threads
-// otherwise (one scalar access covers 128 bytes a warp, which are one block of a checkpoint).
+// otherwise (one scalar access covers 128 bytes of a warp, and 32 / T of them by a narrower team are one block of a checkpoint).
 template <int T, bool VEC>
 __device__ __forceinline__ int col_of(int v, int k, int t) {
   return VEC ? 4 * (v * T + t) + k : (4 * v + k) * T + t;
@@ -31,7 +31,7 @@ __device__ __forceinline__ void load_row(const float* row, int f, int t, float (
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {
-      const int c = 4 * (v * T + t);
+      const int c = col_of<T, VEC>(v, 0, t);
       const float4 a = c < f ? *reinterpret_cast<const float4*>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
       x[4 * v] = a.x;
       x[4 * v + 1] = a.y;
@@ -40,7 +40,7 @@ __device__ __forceinline__ void load_row(const float* row, int f, int t, float (
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = (4 * v + k) * T + t;
+        const int c = col_of<T, VEC>(v, k, t);
         x[4 * v + k] = c < f ? row[c] : 0.f;
       }
     }
@@ -59,7 +59,7 @@ __device__ __forceinline__ void store_row(float* row, int f, int n_pad, int t, c
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {
-      const int c = 4 * (v * T + t);
+      const int c = col_of<T, VEC>(v, 0, t);
       float4 a = make_float4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
       if (f & 3) {
         a.y = c + 1 < f ? a.y : 0.f;
@@ -70,7 +70,7 @@ __device__ __forceinline__ void store_row(float* row, int f, int n_pad, int t, c
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = (4 * v + k) * T + t;
+        const int c = col_of<T, VEC>(v, k, t);
         if (c < n_pad) row[c] = c < f ? x[4 * v + k] : 0.f;
       }
     }
@@ -90,7 +90,7 @@ __device__ __forceinline__ void load_packed(const PackedRows& p, int64_t row, in
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {
-      const int c = 4 * (v * T + t);
+      const int c = col_of<T, VEC>(v, 0, t);
       const uint32_t q4 = c < f ? *reinterpret_cast<const uint32_t*>(q + c) : 0u;
       const float step = c < f ? pack8_step(e[c / kPackBlock]) : 0.f;
       float a[4];
@@ -100,7 +100,7 @@ __device__ __forceinline__ void load_packed(const PackedRows& p, int64_t row, in
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = (4 * v + k) * T + t;
+        const int c = col_of<T, VEC>(v, k, t);
         x[4 * v + k] = c < f ? (float)q[c] * pack8_step(e[c / kPackBlock]) : 0.f;
       }
     }
@@ -115,7 +115,7 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {  // eight lanes hold a block
-      const int c = 4 * (v * T + t);
+      const int c = col_of<T, VEC>(v, 0, t);
       uint32_t m = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) m = max(m, c + k < f ? __float_as_uint(x[4 * v + k]) & 0x7fffffffu : 0u);
@@ -127,10 +127,34 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
       for (int k = 0; k < 4; ++k) b[k] = c + k < f && ex != 255 ? x[4 * v + k] : 0.f;
       if (in && c < f16) *reinterpret_cast<uint32_t*>(q + c) = pack8_bytes(b, ex);
       if (in && c < f && (t & 7) == 0) e[c / kPackBlock] = (uint8_t)ex;
+    } else if constexpr (T < 32) {  // PK values of a team's lanes are a block
+      constexpr int PK = 32 / T;
+#pragma unroll
+      for (int k0 = 0; k0 < 4; k0 += PK) {
+        float a[4] = {0.f, 0.f, 0.f, 0.f};
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < PK; ++k) {
+          a[k] = col_of<T, VEC>(v, k0 + k, t) < f ? x[4 * v + k0 + k] : 0.f;
+          m = max(m, __float_as_uint(a[k]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int o = 1; o < T; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
+        const uint32_t ex = pack8_exponent(m);
+        if (ex == 255) a[0] = a[1] = a[2] = a[3] = 0.f;
+        const uint32_t b = pack8_bytes(a, ex);
+#pragma unroll
+        for (int k = 0; k < PK; ++k) {
+          const int c = col_of<T, VEC>(v, k0 + k, t);
+          if (in && c < f16) q[c] = (int8_t)(b >> (8 * k));
+        }
+        const int c = col_of<T, VEC>(v, k0, t);
+        if (in && c < f && t == 0) e[c / kPackBlock] = (uint8_t)ex;
+      }
     } else {  // a warp holds a block
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = (4 * v + k) * T + t;
+        const int c = col_of<T, VEC>(v, k, t);
         const float a = c < f ? x[4 * v + k] : 0.f;
         const uint32_t ex = pack8_exponent(__reduce_max_sync(kFull, __float_as_uint(a) & 0x7fffffffu));
         const float b[4] = {ex == 255 ? 0.f : a, 0.f, 0.f, 0.f};
@@ -153,17 +177,32 @@ __device__ __forceinline__ void store_bits(const BitRows& p, int64_t row, bool i
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {
-      const int c = 4 * (v * T + t);
+      const int c = col_of<T, VEC>(v, 0, t);
       uint32_t b = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) b |= (c + k < f && y[4 * v + k] > 0.f ? 1u : 0u) << ((c + k) & 31);
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) b |= __shfl_xor_sync(kFull, b, o);
       if (in && c < f && (t & 7) == 0) w[c / 32] = b;
+    } else if constexpr (T < 32) {
+      constexpr int PK = 32 / T;
+#pragma unroll
+      for (int k0 = 0; k0 < 4; k0 += PK) {
+        uint32_t b = 0;
+#pragma unroll
+        for (int k = 0; k < PK; ++k) {
+          const int c = col_of<T, VEC>(v, k0 + k, t);
+          b |= (c < f && y[4 * v + k0 + k] > 0.f ? 1u : 0u) << (c & 31);
+        }
+#pragma unroll
+        for (int o = 1; o < T; o <<= 1) b |= __shfl_xor_sync(kFull, b, o);
+        const int c = col_of<T, VEC>(v, k0, t);
+        if (in && c < f && t == 0) w[c / 32] = b;
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = (4 * v + k) * T + t;
+        const int c = col_of<T, VEC>(v, k, t);
         const uint32_t b = __ballot_sync(kFull, c < f && y[4 * v + k] > 0.f);
         if (in && c < f && (t & 31) == 0) w[c / 32] = b;
       }
@@ -211,14 +250,20 @@ __device__ __forceinline__ void load_cols(const float* __restrict__ w, float non
 
 // The mean is corrected by the mean of what is left after subtracting it, and the variance is taken around the corrected
 // one: a column offset of 1e4 next to a spread of 1 then costs no digits, as the differences x - mean are exact.
+//
+// A short row is the chain load - two sums across lanes - store: a warp that holds few float4 of a row works on R at a time
+// (200 000 x 100: 66 us with one, 56 with four).  The rest is registers, for enough warps: 83 194 x 601 takes 147 us with 172 a
+// thread, 99 with 128 and a few spilled; 48 543 x 1 030 by 4-byte accesses 433 with 148, 168 with 64.
+GCNSA_HD constexpr int norm_rows_at_once(int t, int nv) { return t > 32 ? 1 : t < 32 ? 2 : nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+constexpr int norm_blocks_per_sm(int t, int nv) { return nv <= 2 ? 4 : t <= 32 && nv <= 4 ? 3 : 2; }
 template <int T, int NV, bool VEC>
-__global__ void __launch_bounds__(kNormThreads)
+__global__ void __launch_bounds__(kNormThreads, norm_blocks_per_sm(T, NV))
 layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __restrict__ gamma, const float* __restrict__ beta,
                 float eps, int relu, float* y, int64_t ldy, float* __restrict__ mean_out, float* __restrict__ rstd_out,
                 PackedRows x8, PackedRows y8, BitRows bits) {
   wait_for_predecessors();
-  __shared__ float sh1[2][1][kNormThreads / 32], sh2[2][2][kNormThreads / 32];
-  constexpr int TEAMS = kNormThreads / T;
+  constexpr int R = norm_rows_at_once(T, NV), TEAMS = kNormThreads / T;
+  __shared__ float sh1[2][R][kNormThreads / 32], sh2[2][2 * R][kNormThreads / 32];
   const int t = threadIdx.x % T, team = threadIdx.x / T;
   const int n_pad = (int)min(ldy, (int64_t)((f + 3) / 4 * 4));
   const float inv_f = 1.f / (float)f;
@@ -227,41 +272,55 @@ layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __re
   load_cols<T, NV, VEC>(gamma, 1.f, f, t, ga);
   load_cols<T, NV, VEC>(beta, 0.f, f, t, be);
   // all lanes of a warp stay together (shuffles): rows past the end are computed on zeros and not written
-  for (int64_t base = (int64_t)blockIdx.x * TEAMS; base < n; base += (int64_t)gridDim.x * TEAMS) {
-    const int64_t row = base + team;
-    const bool in = row < n;
-    float a[4 * NV];
-    load_row<T, NV, VEC>(x + row * ldx, in ? f : 0, t, a);
-    clear_pads<T, NV, VEC>(f, t, a);
-    if (x8.q) store_packed<T, NV, VEC>(x8, row, in, f, t, a);
-    float s[1] = {0.f};
+  for (int64_t base = (int64_t)blockIdx.x * TEAMS * R; base < n; base += (int64_t)gridDim.x * TEAMS * R) {
+    float a[R][4 * NV], s[R], d[2 * R];
 #pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) s[0] += a[i];
-    team_sum<T, 1>(s, sh1, s1);
-    const float m0 = s[0] * inv_f;
-    float d[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) {
-      a[i] = col_of<T, VEC>(i / 4, i % 4, t) < f ? a[i] - m0 : 0.f;
-      d[0] += a[i];
-      d[1] = fmaf(a[i], a[i], d[1]);
+    for (int q = 0; q < R; ++q) {
+      const int64_t row = base + q * TEAMS + team;
+      load_row<T, NV, VEC>(x + row * ldx, row < n ? f : 0, t, a[q]);
     }
-    team_sum<T, 2>(d, sh2, s2);
-    const float dm = d[0] * inv_f;
-    // (max drops a NaN, which has to reach rstd)
-    const float var = fmaf(-dm, dm, d[1] * inv_f), r = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);
 #pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) a[i] = norm_value((a[i] - dm) * r, ga[i], be[i]);
-    if (relu)
+    for (int q = 0; q < R; ++q) {
+      const int64_t row = base + q * TEAMS + team;
+      clear_pads<T, NV, VEC>(f, t, a[q]);
+      if (x8.q) store_packed<T, NV, VEC>(x8, row, row < n, f, t, a[q]);
+      s[q] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4 * NV; ++i) a[i] = a[i] < 0.f ? 0.f : a[i];
-    if (y8.q) store_packed<T, NV, VEC>(y8, row, in, f, t, a);
-    if (bits.w) store_bits<T, NV, VEC>(bits, row, in, f, t, a);
-    if (in) {
-      store_row<T, NV, VEC>(y + row * ldy, f, n_pad, t, a);
-      if (t == 0) {
-        if (mean_out) mean_out[row] = m0 + dm;
-        if (rstd_out) rstd_out[row] = r;
+      for (int i = 0; i < 4 * NV; ++i) s[q] += a[q][i];
+    }
+    team_sum<T, R>(s, sh1, s1);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const float m0 = s[q] * inv_f;
+      d[2 * q] = d[2 * q + 1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4 * NV; ++i) {
+        a[q][i] = col_of<T, VEC>(i / 4, i % 4, t) < f ? a[q][i] - m0 : 0.f;
+        d[2 * q] += a[q][i];
+        d[2 * q + 1] = fmaf(a[q][i], a[q][i], d[2 * q + 1]);
+      }
+    }
+    team_sum<T, 2 * R>(d, sh2, s2);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const int64_t row = base + q * TEAMS + team;
+      const bool in = row < n;
+      const float dm = d[2 * q] * inv_f;
+      // (max drops a NaN, which has to reach rstd)
+      const float var = fmaf(-dm, dm, d[2 * q + 1] * inv_f), r = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);
+#pragma unroll
+      for (int i = 0; i < 4 * NV; ++i) a[q][i] = norm_value((a[q][i] - dm) * r, ga[i], be[i]);
+      if (relu)
+#pragma unroll
+        for (int i = 0; i < 4 * NV; ++i) a[q][i] = a[q][i] < 0.f ? 0.f : a[q][i];
+      if (y8.q) store_packed<T, NV, VEC>(y8, row, in, f, t, a[q]);
+      if (bits.w) store_bits<T, NV, VEC>(bits, row, in, f, t, a[q]);
+      if (in) {
+        store_row<T, NV, VEC>(y + row * ldy, f, n_pad, t, a[q]);
+        if (t == 0) {
+          if (mean_out) mean_out[row] = s[q] * inv_f + dm;
+          if (rstd_out) rstd_out[row] = r;
+        }
       }
     }
   }
@@ -282,8 +341,8 @@ __device__ __forceinline__ bool norm_positive(float x, float mean, float rstd, f
 // dx = rstd (u - mean(u) - xh mean(u xh)), u = g gamma where the ReLU let the value through; every block leaves the column
 // sums of g xh and g over its rows in its row of `partial` (2 f floats), which norm_sums adds in block order.
 //
-// Registers decide how many rows are on the way: with 127 a thread (the compiler's choice for NV = 2) two blocks an SM, 269 498 x
-// 256 takes 158 us; at most 80 make it three, 148.  (The next row's loads before this row's sums: 156, with spills 214.)
+// Registers decide how many rows are on the way: with 127 a thread (the compiler's choice for T = 32, NV = 2) two blocks an SM,
+// 269 498 x 256 takes 158 us; at most 80 make it three, 148.  (The next row's loads before this row's sums: 156.)
 constexpr int grad_blocks_per_sm(int nv) { return nv <= 1 ? 4 : nv <= 2 ? 3 : nv <= 4 ? 2 : 1; }
 template <int T, int NV, bool VEC, bool X8>
 __global__ void __launch_bounds__(kNormThreads, grad_blocks_per_sm(NV))
@@ -679,16 +738,27 @@ bool vec_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld
 PackedRows rows_of(const gcnsa_packed8* p) {
   return p ? PackedRows{p->q, p->ldq, p->e, p->lde} : PackedRows{};
 }
-// blocks of a kernel whose teams take a row at a time
-int norm_blocks(int64_t n, int teams, int most) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + teams - 1) / teams, most)); }
-int grad_teams(int32_t f) { return f <= kNarrowCols ? kNormThreads : f <= 32 ? 32 : f <= 64 ? 16 : f <= 512 ? 8 : 1; }
-// (float4 of a row to a thread, as launch_layer_norm_grad has it)
-int grad_nv(int32_t f) { return f <= 128 ? 1 : f <= 256 ? 2 : f <= 512 ? 4 : f <= 1024 ? 1 : f <= 2048 ? 2 : f <= 4096 ? 4 : 8; }
+// How a row of f columns is held: threads of a team, and float4 of it to each.  Lanes of a warp as far as registers go (up to
+// `lane_vecs` float4 each, backward twice as many values are kept): a block's barriers cost a row more than its waiting
+// lanes (50 003 x 1 001 forward: 72 us with a warp to a row, 228 with a block).
+struct RowTeam {
+  int t, nv;
+};
+constexpr int kNormLaneVecs = 8, kGradLaneVecs = 4;
+RowTeam row_team(int32_t f, int lane_vecs) {
+  const int vecs = (f + 3) / 4, lane = (vecs + 31) / 32, thread = (vecs + kNormThreads - 1) / kNormThreads;
+  if (vecs <= 16) return {vecs <= 8 ? 8 : 16, 1};
+  if (lane <= lane_vecs) return {32, lane <= 4 ? lane : lane <= 6 ? 6 : 8};
+  return {kNormThreads, thread <= 2 ? thread : thread <= 4 ? 4 : 8};
+}
+int row_blocks(int64_t n, int64_t rows_per_block, int64_t most) { return (int)std::max<int64_t>(1, std::min((n + rows_per_block - 1) / rows_per_block, most)); }
+// blocks of the backward pass; sizes alone decide (the scratch holds a line for each)
 int grad_blocks(int64_t n, int32_t f) {
+  if (f <= kNarrowCols) return row_blocks(n, kNormThreads, 148 * 4);
   // rows too wide for registers: a block's partial sums are as wide, and all of them take at most 256 MB
-  const int64_t most = f > kNormMaxCols ? std::max<int64_t>(1, std::min<int64_t>(148 * 4, (int64_t(256) << 20) / (8 * (int64_t)f)))
-                                        : 148 * grad_blocks_per_sm(grad_nv(f));
-  return norm_blocks(n, grad_teams(f), (int)most);
+  if (f > kNormMaxCols) return row_blocks(n, 1, std::max<int64_t>(1, std::min<int64_t>(148 * 4, (int64_t(256) << 20) / (8 * (int64_t)f))));
+  const RowTeam m = row_team(f, kGradLaneVecs);
+  return row_blocks(n, kNormThreads / m.t, 148 * grad_blocks_per_sm(m.nv));
 }
 
 }  // namespace
@@ -700,20 +770,28 @@ int launch_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_
   cudaStream_t s = (cudaStream_t)stream;
   const bool vec = vec_rows(x, ldx) && vec_rows(y, ldy);
   const PackedRows px = rows_of(x8), py = rows_of(y8);
-  auto run = [&](auto kernel, int teams) {
-    launch(kernel, norm_blocks(n, teams, 148 * 8), kNormThreads, 0, s, n, f, x, ldx, gamma, beta, eps, relu, y, ldy, mean, rstd, px, py,
-           BitRows{bits, ldbits});
+  auto run = [&](auto kernel, int blocks) {
+    launch(kernel, blocks, kNormThreads, 0, s, n, f, x, ldx, gamma, beta, eps, relu, y, ldy, mean, rstd, px, py, BitRows{bits, ldbits});
   };
-  if (f > kNormMaxCols) run(layer_norm_wide, 1);
-  else if (vec && f <= 32) run(layer_norm_rows<8, 1, true>, 32);
-  else if (vec && f <= 64) run(layer_norm_rows<16, 1, true>, 16);
-  else if (f <= 128) vec ? run(layer_norm_rows<32, 1, true>, 8) : run(layer_norm_rows<32, 1, false>, 8);
-  else if (f <= 256) vec ? run(layer_norm_rows<32, 2, true>, 8) : run(layer_norm_rows<32, 2, false>, 8);
-  else if (f <= 512) vec ? run(layer_norm_rows<32, 4, true>, 8) : run(layer_norm_rows<32, 4, false>, 8);
-  else if (f <= 1024) vec ? run(layer_norm_rows<32, 8, true>, 8) : run(layer_norm_rows<32, 8, false>, 8);
-  else if (f <= 2048) vec ? run(layer_norm_rows<256, 2, true>, 1) : run(layer_norm_rows<256, 2, false>, 1);
-  else if (f <= 4096) vec ? run(layer_norm_rows<256, 4, true>, 1) : run(layer_norm_rows<256, 4, false>, 1);
-  else vec ? run(layer_norm_rows<256, 8, true>, 1) : run(layer_norm_rows<256, 8, false>, 1);
+  if (f > kNormMaxCols) {
+    run(layer_norm_wide, row_blocks(n, 1, 148 * 8));
+  } else {
+    const RowTeam m = row_team(f, kNormLaneVecs);
+    const int blocks = row_blocks(n, kNormThreads / m.t * norm_rows_at_once(m.t, m.nv), 148 * 8);
+#define GCNSA_NORM(T, NV) (vec ? run(layer_norm_rows<T, NV, true>, blocks) : run(layer_norm_rows<T, NV, false>, blocks))
+    if (m.t == 8) GCNSA_NORM(8, 1);
+    else if (m.t == 16) GCNSA_NORM(16, 1);
+    else if (m.t == 32 && m.nv == 1) GCNSA_NORM(32, 1);
+    else if (m.t == 32 && m.nv == 2) GCNSA_NORM(32, 2);
+    else if (m.t == 32 && m.nv == 3) GCNSA_NORM(32, 3);
+    else if (m.t == 32 && m.nv == 4) GCNSA_NORM(32, 4);
+    else if (m.t == 32 && m.nv == 6) GCNSA_NORM(32, 6);
+    else if (m.t == 32) GCNSA_NORM(32, 8);
+    else if (m.nv == 2) GCNSA_NORM(256, 2);
+    else if (m.nv == 4) GCNSA_NORM(256, 4);
+    else GCNSA_NORM(256, 8);
+#undef GCNSA_NORM
+  }
   note_launch();
   return (int)cudaGetLastError();
 }
@@ -731,26 +809,27 @@ int launch_layer_norm_grad(void* stream, int64_t n, int32_t f, const float* g, i
     const bool vec = (x8 || vec_rows(x, ldx)) && vec_rows(g, ldg) && vec_rows(dx, lddx);
     const PackedRows p = rows_of(x8);
     const BitRows through{const_cast<uint32_t*>(bits), ldbits};
+    const RowTeam m = row_team(f, kGradLaneVecs);
     auto run = [&](auto kernel) {
       launch(kernel, blocks, kNormThreads, 0, s, n, f, g, ldg, x, ldx, p, mean, rstd, gamma, beta, relu, through, dx, lddx, partial);
     };
-    // (the number of blocks is that of grad_teams; a kernel with other teams strides over the rows all the same)
 #define GCNSA_NORM_GRAD(T, NV)                                                                                        \
   (vec ? (x8 ? run(layer_norm_grad<T, NV, true, true>) : run(layer_norm_grad<T, NV, true, false>))                    \
        : (x8 ? run(layer_norm_grad<T, NV, false, true>) : run(layer_norm_grad<T, NV, false, false>)))
     if (f <= kNarrowCols) x8 ? run(layer_norm_grad_narrow<true>) : run(layer_norm_grad_narrow<false>);
-    else if (vec && f <= 32) x8 ? run(layer_norm_grad<8, 1, true, true>) : run(layer_norm_grad<8, 1, true, false>);
-    else if (vec && f <= 64) x8 ? run(layer_norm_grad<16, 1, true, true>) : run(layer_norm_grad<16, 1, true, false>);
-    else if (f <= 128) GCNSA_NORM_GRAD(32, 1);
-    else if (f <= 256) GCNSA_NORM_GRAD(32, 2);
-    else if (f <= 512) GCNSA_NORM_GRAD(32, 4);
-    else if (f <= 1024) GCNSA_NORM_GRAD(256, 1);
-    else if (f <= 2048) GCNSA_NORM_GRAD(256, 2);
-    else if (f <= 4096) GCNSA_NORM_GRAD(256, 4);
-    else if (f <= kNormMaxCols) GCNSA_NORM_GRAD(256, 8);
-    else
+    else if (f > kNormMaxCols)
       launch(layer_norm_grad_wide, blocks, kNormThreads, 0, s, n, f, g, ldg, WideRow{x, ldx, p}, mean, rstd, gamma, beta, relu,
              through, dx, lddx, partial);
+    else if (m.t == 8) GCNSA_NORM_GRAD(8, 1);
+    else if (m.t == 16) GCNSA_NORM_GRAD(16, 1);
+    else if (m.t == 32 && m.nv == 1) GCNSA_NORM_GRAD(32, 1);
+    else if (m.t == 32 && m.nv == 2) GCNSA_NORM_GRAD(32, 2);
+    else if (m.t == 32 && m.nv == 3) GCNSA_NORM_GRAD(32, 3);
+    else if (m.t == 32) GCNSA_NORM_GRAD(32, 4);
+    else if (m.nv == 1) GCNSA_NORM_GRAD(256, 1);
+    else if (m.nv == 2) GCNSA_NORM_GRAD(256, 2);
+    else if (m.nv == 4) GCNSA_NORM_GRAD(256, 4);
+    else GCNSA_NORM_GRAD(256, 8);
 #undef GCNSA_NORM_GRAD
     note_launch();
   }
