@@ -116,15 +116,13 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
   for (int v = 0; v < NV; ++v) {
     if constexpr (VEC) {  // eight lanes hold a block
       const int c = col_of<T, VEC>(v, 0, t);
-      uint32_t m = 0;
+      float b[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) m = max(m, c + k < f ? __float_as_uint(x[4 * v + k]) & 0x7fffffffu : 0u);
+      for (int k = 0; k < 4; ++k) b[k] = c + k < f ? x[4 * v + k] : 0.f;
+      uint32_t m = pack8_magnitude(b);
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
       const uint32_t ex = pack8_exponent(m);
-      float b[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) b[k] = c + k < f && ex != 255 ? x[4 * v + k] : 0.f;
       if (in && c < f16) *reinterpret_cast<uint32_t*>(q + c) = pack8_bytes(b, ex);
       if (in && c < f && (t & 7) == 0) e[c / kPackBlock] = (uint8_t)ex;
     } else if constexpr (T < 32) {  // PK values of a team's lanes are a block
@@ -132,16 +130,12 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
 #pragma unroll
       for (int k0 = 0; k0 < 4; k0 += PK) {
         float a[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < PK; ++k) {
-          a[k] = col_of<T, VEC>(v, k0 + k, t) < f ? x[4 * v + k0 + k] : 0.f;
-          m = max(m, __float_as_uint(a[k]) & 0x7fffffffu);
-        }
+        for (int k = 0; k < PK; ++k) a[k] = col_of<T, VEC>(v, k0 + k, t) < f ? x[4 * v + k0 + k] : 0.f;
+        uint32_t m = pack8_magnitude(a);
 #pragma unroll
         for (int o = 1; o < T; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
         const uint32_t ex = pack8_exponent(m);
-        if (ex == 255) a[0] = a[1] = a[2] = a[3] = 0.f;
         const uint32_t b = pack8_bytes(a, ex);
 #pragma unroll
         for (int k = 0; k < PK; ++k) {
@@ -157,7 +151,7 @@ __device__ __forceinline__ void store_packed(const PackedRows& p, int64_t row, b
         const int c = col_of<T, VEC>(v, k, t);
         const float a = c < f ? x[4 * v + k] : 0.f;
         const uint32_t ex = pack8_exponent(__reduce_max_sync(kFull, __float_as_uint(a) & 0x7fffffffu));
-        const float b[4] = {ex == 255 ? 0.f : a, 0.f, 0.f, 0.f};
+        const float b[4] = {a, 0.f, 0.f, 0.f};
         if (in && c < f16) q[c] = (int8_t)pack8_bytes(b, ex);
         if (in && c < f && (t & 31) == 0) e[c / kPackBlock] = (uint8_t)ex;
       }
@@ -646,19 +640,22 @@ struct BlockWalk {
     }
   }
 };
-// UNROLL blocks of a lane are on the way at a time; reading bytes takes twice as many of them to fill the time to memory.
-template <bool VEC, int UNROLL>
-__global__ void __launch_bounds__(256)
+// kPackUnroll blocks of a lane are on the way at a time, and the grid is what the SMs hold at once.  552 000 x 256: packing takes
+// 126 us with six blocks an SM (40 registers), 135 with a grid of eight of which five fit, 147 with eight (32, spilled);
+// unpacking 129 with five blocks of four and four blocks of eight, 150 with eight at a time and three blocks.
+constexpr int kPackUnroll = 4, kPackBlocks = 6, kUnpackBlocks = 5;
+template <bool VEC>
+__global__ void __launch_bounds__(256, kPackBlocks)
 pack8_rows(uint32_t n, int f, int nb, const float* __restrict__ x, int64_t ldx, PackedRows p) {
   wait_for_predecessors();
   const int g = threadIdx.x & 7, f16 = (f + 15) / 16 * 16;
   BlockWalk at(nb, ((uint64_t)blockIdx.x * 256 + threadIdx.x) / 8, (uint64_t)gridDim.x * 32);
   // (a warp's four groups run on together until the last of them is past the end)
   while (__any_sync(kFull, at.row < n)) {
-    float a[UNROLL][4];
+    float a[kPackUnroll][4];
     BlockWalk to = at;
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
+    for (int i = 0; i < kPackUnroll; ++i) {
       const int c = 32 * at.b + 4 * g;
       const float* src = x + at.row * ldx + c;
       if constexpr (VEC) {
@@ -674,14 +671,11 @@ pack8_rows(uint32_t n, int f, int nb, const float* __restrict__ x, int64_t ldx, 
       at.next();
     }
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) m = max(m, __float_as_uint(a[i][k]) & 0x7fffffffu);
+    for (int i = 0; i < kPackUnroll; ++i) {
+      uint32_t m = pack8_magnitude(a[i]);
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
       const uint32_t ex = pack8_exponent(m);
-      if (ex == 255) a[i][0] = a[i][1] = a[i][2] = a[i][3] = 0.f;
       const int c = 32 * to.b + 4 * g;
       if (to.row < n) {
         if (c < f16) *reinterpret_cast<uint32_t*>(p.q + to.row * p.ldq + c) = pack8_bytes(a[i], ex);
@@ -691,17 +685,17 @@ pack8_rows(uint32_t n, int f, int nb, const float* __restrict__ x, int64_t ldx, 
     }
   }
 }
-template <bool VEC, int UNROLL>
-__global__ void __launch_bounds__(256)
+template <bool VEC>
+__global__ void __launch_bounds__(256, kUnpackBlocks)
 unpack8_rows(uint32_t n, int f, int nb, PackedRows p, float* __restrict__ x, int64_t ldx) {
   wait_for_predecessors();
   const int g = threadIdx.x & 7, n_pad = (int)min(ldx, (int64_t)f + (4 - f % 4) % 4);
   BlockWalk at(nb, ((uint64_t)blockIdx.x * 256 + threadIdx.x) / 8, (uint64_t)gridDim.x * 32);
   while (at.row < n) {
-    uint32_t q[UNROLL], ex[UNROLL];
+    uint32_t q[kPackUnroll], ex[kPackUnroll];
     BlockWalk to = at;
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
+    for (int i = 0; i < kPackUnroll; ++i) {
       const int c = 32 * at.b + 4 * g;
       const bool in = at.row < n && c < f;
       q[i] = in ? __ldg(reinterpret_cast<const uint32_t*>(p.q + at.row * p.ldq + c)) : 0u;
@@ -709,7 +703,7 @@ unpack8_rows(uint32_t n, int f, int nb, PackedRows p, float* __restrict__ x, int
       at.next();
     }
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
+    for (int i = 0; i < kPackUnroll; ++i) {
       const int c = 32 * to.b + 4 * g;
       if (to.row < n && c < f) {
         float a[4];
@@ -840,23 +834,22 @@ int launch_layer_norm_grad(void* stream, int64_t n, int32_t f, const float* g, i
   return (int)cudaGetLastError();
 }
 
-constexpr int kPackUnroll = 4, kUnpackUnroll = 8;
-static int pack_blocks(int64_t groups, int unroll) { return (int)std::max<int64_t>(1, std::min<int64_t>((groups + 32 * unroll - 1) / (32 * unroll), 148 * 8)); }
+static int pack_blocks(int64_t groups, int per_sm) { return row_blocks(groups, 32 * kPackUnroll, 148 * per_sm); }
 
 int launch_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p) {
   if (n <= 0) return 0;
-  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb, kPackUnroll);
+  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb, kPackBlocks);
   auto run = [&](auto kernel) { launch(kernel, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, x, ldx, rows_of(p)); };
-  vec_rows(x, ldx) ? run(pack8_rows<true, kPackUnroll>) : run(pack8_rows<false, kPackUnroll>);
+  vec_rows(x, ldx) ? run(pack8_rows<true>) : run(pack8_rows<false>);
   note_launch();
   return (int)cudaGetLastError();
 }
 
 int launch_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx) {
   if (n <= 0) return 0;
-  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb, kUnpackUnroll);
+  const int nb = (f + kPackBlock - 1) / kPackBlock, blocks = pack_blocks(n * nb, kUnpackBlocks);
   auto run = [&](auto kernel) { launch(kernel, blocks, 256, 0, (cudaStream_t)stream, n, f, nb, rows_of(p), x, ldx); };
-  vec_rows(x, ldx) ? run(unpack8_rows<true, kUnpackUnroll>) : run(unpack8_rows<false, kUnpackUnroll>);
+  vec_rows(x, ldx) ? run(unpack8_rows<true>) : run(unpack8_rows<false>);
   note_launch();
   return (int)cudaGetLastError();
 }

@@ -22,21 +22,28 @@ __device__ __forceinline__ uint32_t pack8_exponent(uint32_t bits) {
   // would round to 128
   return (uint32_t)min(max((int)((bits + 0x10000u) >> 23) - 6, 1), 248);
 }
-// 1 / step; 0 for a block that is not finite
-__device__ __forceinline__ float pack8_inverse(uint32_t e) { return e == 255 ? 0.f : __uint_as_float((254 - e) << 23); }
+// the larger of two magnitudes as such a word; a NaN stays one
+__device__ __forceinline__ float pack8_larger(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return m;
+}
+__device__ __forceinline__ uint32_t pack8_magnitude(const float (&x)[4]) {
+  return __float_as_uint(pack8_larger(pack8_larger(x[0], x[1]), pack8_larger(x[2], x[3])));
+}
 __device__ __forceinline__ float pack8_step(uint32_t e) { return __uint_as_float(e << 23); }
-// Four values as bytes: rint(x * inv) is the low byte of x * inv + 1.5 2^23 (x * inv is exact and below 128; ties to even).  x is 0
+// Four values as bytes: rint(x / step) is the low byte of x / step + 1.5 2^23 (x / step is exact and below 128; ties to even); zeros
 // where the block is not finite.
 __device__ __forceinline__ uint32_t pack8_bytes(const float (&x)[4], uint32_t e) {
-  const float inv = pack8_inverse(e);
-  uint32_t b[4];
+  const float inv = __uint_as_float((254 - e) << 23);
+  float s[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    float s = x[k] * inv;
-    if (e == 248) s = fminf(fmaxf(s, -127.f), 127.f);
-    b[k] = __float_as_uint(s + 12582912.f);
-  }
-  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  for (int k = 0; k < 4; ++k) s[k] = fmaf(x[k], inv, 12582912.f);
+  if (e >= 248)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = e == 255 ? 0.f : fminf(fmaxf(s[k], 12582912.f - 127.f), 12582912.f + 127.f);
+  return __byte_perm(__byte_perm(__float_as_uint(s[0]), __float_as_uint(s[1]), 0x0040),
+                     __byte_perm(__float_as_uint(s[2]), __float_as_uint(s[3]), 0x0040), 0x5410);
 }
 // four packed bytes as floats: 2^23 + (q + 128) has q + 128 as its low byte
 __device__ __forceinline__ void pack8_open(uint32_t q4, float (&v)[4]) {
