@@ -247,7 +247,8 @@ __device__ __forceinline__ void load_cols(const float* __restrict__ w, float non
 //
 // A short row is the chain load - two sums across lanes - store: a warp that holds few float4 of a row works on R at a time
 // (200 000 x 100: 66 us with one, 56 with four).  The rest is registers, for enough warps: 83 194 x 601 takes 147 us with 172 a
-// thread, 99 with 128 and a few spilled; 48 543 x 1 030 by 4-byte accesses 433 with 148, 168 with 64.
+// thread, 94 with 128 and a few spilled; 48 543 x 1 030 by 4-byte accesses 433 with 148, 168 with 64.  The grid is what the SMs
+// hold at once (twice as many blocks: 83 194 x 601 96, 50 003 x 1 001 72 for 70).
 GCNSA_HD constexpr int norm_rows_at_once(int t, int nv) { return t > 32 ? 1 : t < 32 ? 2 : nv == 1 ? 4 : nv == 2 ? 2 : 1; }
 constexpr int norm_blocks_per_sm(int t, int nv) { return nv <= 2 ? 4 : t <= 32 && nv <= 4 ? 3 : 2; }
 template <int T, int NV, bool VEC>
@@ -734,7 +735,7 @@ PackedRows rows_of(const gcnsa_packed8* p) {
 }
 // How a row of f columns is held: threads of a team, and float4 of it to each.  Lanes of a warp as far as registers go (up to
 // `lane_vecs` float4 each, backward twice as many values are kept): a block's barriers cost a row more than its waiting
-// lanes (50 003 x 1 001 forward: 72 us with a warp to a row, 228 with a block).
+// lanes (50 003 x 1 001 forward: 70 us with a warp to a row, 228 with a block).
 struct RowTeam {
   int t, nv;
 };
@@ -771,7 +772,7 @@ int launch_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_
     run(layer_norm_wide, row_blocks(n, 1, 148 * 8));
   } else {
     const RowTeam m = row_team(f, kNormLaneVecs);
-    const int blocks = row_blocks(n, kNormThreads / m.t * norm_rows_at_once(m.t, m.nv), 148 * 8);
+    const int blocks = row_blocks(n, kNormThreads / m.t * norm_rows_at_once(m.t, m.nv), 148 * norm_blocks_per_sm(m.t, m.nv));
 #define GCNSA_NORM(T, NV) (vec ? run(layer_norm_rows<T, NV, true>, blocks) : run(layer_norm_rows<T, NV, false>, blocks))
     if (m.t == 8) GCNSA_NORM(8, 1);
     else if (m.t == 16) GCNSA_NORM(16, 1);
