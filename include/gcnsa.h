@@ -622,7 +622,11 @@ int gcnsa_op_colsum_static(void* stream, int64_t n, int32_t f, const float* g, i
  * For models beyond the paper's two layers (it stacks up to a few, Section 4.1):
  * a norm between layers, hidden rows kept in 8 bits until the backward pass, and
  * a loss whose logits are never stored.  Results whose leading dimension leaves
- * room have zeros in the pad columns up to the next multiple of 4. */
+ * room have zeros in the pad columns up to the next multiple of 4, in the last
+ * row too (so a result is not a window of a wider matrix unless the pad columns
+ * belong to it).  A workspace or scratch is in use until the kernels of its call
+ * have run: calls (and captured graphs) that may run at the same time need one
+ * each. */
 
 /* A checkpoint of n rows of f columns.  Every 32 columns of a row share a step
  * 2^(e - 127); a value is q * step, q in [-127, 127].  e is the smallest byte
@@ -667,13 +671,13 @@ int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float
                                  int32_t accumulate, void* scratch, size_t scratch_bytes);
 size_t gcnsa_op_layer_norm_backward_scratch(int64_t n, int32_t f);
 
-/* Make a checkpoint of x, and restore one.  n < 2^31. */
+/* Make a checkpoint of x, and restore one.  n, f < 2^31 - 2^17. */
 int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p);
 int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx);
 
 /* dw (+)= X^T G with X [n x f] a checkpoint and G [n x c]: the weight gradient of a
  * layer whose input was kept in 8 bits.  fp32-level accuracy with respect to the
- * values the checkpoint stands for.  n, f, c < 2^31; workspace: DEVICE, 256-byte
+ * values the checkpoint stands for.  n, f, c < 2^31 - 2^17; workspace: DEVICE, 256-byte
  * aligned, gcnsa_op_gemm_packed8_workspace(n, f, c) bytes (NULL when that is 0). */
 int gcnsa_op_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g,
                           int64_t ldg, float* dw, int64_t lddw, int32_t accumulate, void* workspace,
@@ -690,7 +694,7 @@ size_t gcnsa_op_gemm_packed8_workspace(int64_t n, int32_t f, int32_t c);
  * masked rows (n without a mask); with another number the loss comes out as NaN.
  * n_train = 0: loss 0, zero gradients.  Labels of masked rows lie in [0, c); one
  * that does not makes the loss NaN (nothing is read or written out of place).
- * accumulate applies to dw and db.  d, c >= 1; n, d, c < 2^31, n c < 2^45; workspace: DEVICE,
+ * accumulate applies to dw and db.  d, c >= 1; n, d, c < 2^31 - 2^17, n c < 2^45; workspace: DEVICE,
  * 256-byte aligned, gcnsa_op_linear_ce_workspace(n, d, c) bytes. */
 int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const float* h, int64_t ldh, const float* w,
                        int64_t ldw, const float* bias, const int32_t* y, const uint8_t* mask, int64_t n_train,

@@ -1607,6 +1607,9 @@ int gcnsa_op_colsum_scaled(void* stream, int64_t n, int32_t f, const float* g, i
   return GCNSA_OK;
 }
 
+// Rows and columns of checkpoints, their products and output layers: kernels round them up to tiles and step beyond them in 32 bits.
+static const int64_t kMostRows = INT32_MAX - (int64_t(1) << 17);
+
 // NULL when the checkpoint can be used, else what is wrong with it
 static const char* packed_fault(const gcnsa_packed8* p, int32_t f) {
   if (!p->q || !p->e) return "NULL pointer in a checkpoint";
@@ -1656,7 +1659,7 @@ int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float
 }
 
 int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const gcnsa_packed8* p) {
-  if (n < 0 || f < 1 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension or f < 1");
+  if (n < 0 || f < 1 || n > kMostRows || f > kMostRows) return fail(GCNSA_ERR_ARG, "negative or oversized dimension or f < 1");
   if (n == 0) return GCNSA_OK;
   if (!x || !p) return fail(GCNSA_ERR_ARG, "NULL pointer");
   if (ldx < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");
@@ -1666,7 +1669,7 @@ int gcnsa_op_pack8(void* stream, int64_t n, int32_t f, const float* x, int64_t l
 }
 
 int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p, float* x, int64_t ldx) {
-  if (n < 0 || f < 1 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension or f < 1");
+  if (n < 0 || f < 1 || n > kMostRows || f > kMostRows) return fail(GCNSA_ERR_ARG, "negative or oversized dimension or f < 1");
   if (n == 0) return GCNSA_OK;
   if (!x || !p) return fail(GCNSA_ERR_ARG, "NULL pointer");
   if (ldx < f) return fail(GCNSA_ERR_ARG, "leading dimension too small");
@@ -1683,7 +1686,7 @@ size_t gcnsa_op_gemm_packed8_workspace(int64_t n, int32_t f, int32_t c) {
 
 int gcnsa_op_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g, int64_t ldg,
                           float* dw, int64_t lddw, int32_t accumulate, void* workspace, size_t workspace_bytes) {
-  if (n < 0 || f < 0 || c < 0 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension");
+  if (n < 0 || f < 0 || c < 0 || n > kMostRows || f > kMostRows || c > kMostRows) return fail(GCNSA_ERR_ARG, "negative or oversized dimension");
   if (f == 0 || c == 0) return GCNSA_OK;
   if (!dw || (n > 0 && (!x || !g))) return fail(GCNSA_ERR_ARG, "NULL pointer");
   if (lddw < c || (n > 0 && ldg < c)) return fail(GCNSA_ERR_ARG, "leading dimension too small");
@@ -1703,6 +1706,7 @@ int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const floa
                        int64_t lddh, float* dw, int64_t lddw, float* db, int32_t accumulate, void* workspace,
                        size_t workspace_bytes) {
   if (n < 0 || d < 1 || c < 1 || n_train < 0 || n >= INT32_MAX) return fail(GCNSA_ERR_ARG, "negative or oversized dimension, d < 1 or c < 1");
+  if (n > kMostRows || d > kMostRows || c > kMostRows) return fail(GCNSA_ERR_TOO_LARGE, "n, d or c exceeds int32 indexing");
   // tiles of 128 x 128 logits are counted in 32 bits
   if (((n + 127) / 128) * (((int64_t)c + 127) / 128) >= INT32_MAX) return fail(GCNSA_ERR_TOO_LARGE, "n c / 16384 exceeds int32 indexing");
   if (n_train > n || (!mask && n_train != n)) return fail(GCNSA_ERR_ARG, "n_train is the number of masked rows");

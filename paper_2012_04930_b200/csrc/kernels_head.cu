@@ -32,9 +32,10 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <class Cost>
 int cheapest_slices(int64_t tiles, int64_t units, Cost cost) {
   const int most = (int)std::min<int64_t>(units, std::max<int64_t>(1, 2 * sm_count() / tiles));
-  int best = 1, best_cost = INT32_MAX;
+  int best = 1;
+  int64_t best_cost = INT64_MAX;
   for (int s = 1; s <= most; s += std::max(1, s / 16)) {  // (one in 16 apart: the search runs in every call)
-    const int len = (int)div_up(units, s), c = cost((int)div_up(units, len), len);
+    const int64_t len = div_up(units, s), c = cost(div_up(units, len), len);
     if (c < best_cost) {
       best = s;
       best_cost = c;
@@ -43,19 +44,17 @@ int cheapest_slices(int64_t tiles, int64_t units, Cost cost) {
   return (int)div_up(units, div_up(units, best));
 }
 int pick_slices(int64_t tiles, int64_t units) {
-  const int sms = sm_count(), t = (int)tiles;
-  return cheapest_slices(tiles, units, [&](int s, int len) { return (t * s + sms - 1) / sms * (len + 6); });
+  return cheapest_slices(tiles, units, [&](int64_t s, int64_t len) { return div_up(tiles * s, sm_count()) * (len + 6); });
 }
 // The same for a product whose items are followed in a launch by `others` items of other_units k-blocks.  Block b takes items b,
 // b + grid, ...: what the fullest block gets, which is the first one or the first with an item less of either kind.
 int balanced_slices(int64_t tiles, int64_t units, int64_t others, int64_t other_units) {
-  const int sms = sm_count(), t = (int)tiles, o = (int)others;
-  return cheapest_slices(tiles, units, [&](int s, int len) {
-    const int items = t * s, total = items + o, grid = std::min(total, sms);
-    int most = 0;
-    for (const int b : {0, items % grid, total % grid}) {
-      const int mine = items > b ? (items - b + grid - 1) / grid : 0, all = (total - b + grid - 1) / grid;
-      most = std::max(most, mine * (len + 6) + (all - mine) * ((int)other_units + 6));
+  return cheapest_slices(tiles, units, [&](int64_t s, int64_t len) {
+    const int64_t items = tiles * s, total = items + others, grid = std::min<int64_t>(total, sm_count());
+    int64_t most = 0;
+    for (const int64_t b : {int64_t(0), items % grid, total % grid}) {
+      const int64_t mine = items > b ? div_up(items - b, grid) : 0, all = div_up(total - b, grid);
+      most = std::max(most, mine * (len + 6) + (all - mine) * (other_units + 6));
     }
     return most;
   });

@@ -775,8 +775,10 @@ def _vector(t, name, dtype, size, dev):
     return t.data_ptr()
 
 
-def _matrix(t, name, dtype, rows, cols, dev):
-    """(pointer, leading dimension) of a device matrix [rows x at least cols] whose columns are contiguous, or (None, 0)."""
+def _matrix(t, name, dtype, rows, cols, dev, result=False):
+    """(pointer, leading dimension) of a device matrix [rows x at least cols] whose columns are contiguous, or (None, 0).  Rows of a
+    result are written up to the next multiple of 4 columns where the leading dimension leaves room, so these columns have to
+    be the tensor's own."""
     if t is None:
         return None, 0
     shape = t.shape
@@ -784,6 +786,8 @@ def _matrix(t, name, dtype, rows, cols, dev):
             (shape[1] > 1 and t.stride(1) != 1)):
         _refuse(f"{name}: rows of contiguous {dtype} columns on cuda:{dev} are needed, [{rows} x at least {cols}], got {t.dtype} "
                 f"{tuple(shape)} with strides {t.stride() if t.dim() else ()} on {t.device}")
+    if result and rows > 1 and shape[1] < min(t.stride(0), (cols + 3) // 4 * 4):
+        _refuse(f"{name}: a window of {shape[1]} columns in rows of {t.stride(0)}; columns up to {(cols + 3) // 4 * 4} are written (zeros behind {cols})")
     # (the stride of a single row says nothing)
     return t.data_ptr(), t.stride(0) if rows > 1 else max(shape[1], cols)
 
@@ -838,7 +842,7 @@ def op_layer_norm(x, f, y, gamma=None, beta=None, eps=1e-5, relu=0, mean=None, r
     let through."""
     n, dev, stream = _leader(x, "x")
     xp, ldx = _matrix(x, "x", "float32", n, f, dev)
-    yp, ldy = _matrix(y, "y", "float32", n, f, dev)
+    yp, ldy = _matrix(y, "y", "float32", n, f, dev, True)
     bp, ldb = _matrix(bits, "bits", "int32", n, (f + 31) // 32, dev)
     _ck(lib().gcnsa_op_layer_norm(stream, n, f, xp, ldx, _vector(gamma, "gamma", "float32", f, dev), _vector(beta, "beta", "float32", f, dev),
                                   eps, int(relu), yp, ldy, _vector(mean, "mean", "float32", n, dev), _vector(rstd, "rstd", "float32", n, dev),
@@ -851,7 +855,7 @@ def op_layer_norm_backward(g, x, f, dx, mean, rstd, gamma=None, beta=None, relu=
     what the forward pass said of the ReLU (without: taken from x)."""
     n, dev, stream = _leader(g, "g")
     gp, ldg = _matrix(g, "g", "float32", n, f, dev)
-    dxp, lddx = _matrix(dx, "dx", "float32", n, f, dev)
+    dxp, lddx = _matrix(dx, "dx", "float32", n, f, dev, True)
     x8 = x.on("x", n, f, dev) if isinstance(x, Packed8) else None
     xp, ldx = (None, 0) if x8 is not None else _matrix(x, "x", "float32", n, f, dev)
     bp, ldb = _matrix(bits, "bits", "int32", n, (f + 31) // 32, dev)
@@ -876,7 +880,7 @@ def op_pack8(x, p):
 def op_unpack8(p, x):
     """x = what the checkpoint stands for (first p.f columns)."""
     n, dev, stream = _leader(x, "x")
-    xp, ldx = _matrix(x, "x", "float32", n, p.f, dev)
+    xp, ldx = _matrix(x, "x", "float32", n, p.f, dev, True)
     _ck(lib().gcnsa_op_unpack8(stream, n, p.f, p.on("p", n, p.f, dev), xp, ldx))
 
 
@@ -884,7 +888,7 @@ def op_gemm_packed8(p, g, c, dw, accumulate=0, workspace=None):
     """dw (+)= X^T G with X a checkpoint [n x f] and G the first c columns of g."""
     n, dev, stream = _leader(g, "g")
     gp, ldg = _matrix(g, "g", "float32", n, c, dev)
-    dwp, lddw = _matrix(dw, "dw", "float32", p.f, c, dev)
+    dwp, lddw = _matrix(dw, "dw", "float32", p.f, c, dev, True)
     _ck(lib().gcnsa_op_gemm_packed8(stream, n, p.f, c, p.on("p", n, p.f, dev), gp, ldg, dwp, lddw, accumulate,
                                     *_bytes_of(workspace, "workspace", dev)))
 
@@ -899,8 +903,8 @@ def op_linear_ce(h, d, w, c, y, n_train, loss, dh=None, dw=None, db=None, bias=N
     n, dev, stream = _leader(h, "h")
     hp, ldh = _matrix(h, "h", "float32", n, d, dev)
     wp, ldw = _matrix(w, "w", "float32", d, c, dev)
-    dhp, lddh = _matrix(dh, "dh", "float32", n, d, dev)
-    dwp, lddw = _matrix(dw, "dw", "float32", d, c, dev)
+    dhp, lddh = _matrix(dh, "dh", "float32", n, d, dev, True)
+    dwp, lddw = _matrix(dw, "dw", "float32", d, c, dev, True)
     _ck(lib().gcnsa_op_linear_ce(stream, n, d, c, hp, ldh, wp, ldw, _vector(bias, "bias", "float32", c, dev), _vector(y, "y", "int32", n, dev),
                                  _vector(mask, "mask", "uint8", n, dev), n_train, _vector(loss, "loss", "float32", 1, dev), dhp, lddh, dwp,
                                  lddw, _vector(db, "db", "float32", c, dev), accumulate, *_bytes_of(workspace, "workspace", dev)))

@@ -613,3 +613,21 @@ def test_two_streams_with_workspaces_of_their_own():
     for a, b in zip(alone, beside):
         for key in ("loss", "h", "dwo", "dbo", "dgamma", "dbeta", "dw"):
             assert torch.equal(a[key], b[key]), key
+
+
+def test_windows_of_wider_matrices():
+    """Inputs may be windows of any offset; results too where their pad columns are the window's, and nothing beside them changes."""
+    n, f = 301, 45
+    big = _rand(1, n, 200)
+    x = big[:, 3:3 + f]
+    out = torch.full((n, 200), 7.0, device="cuda")
+    with pytest.raises(gcnsa.GcnsaError):
+        gcnsa.op_layer_norm(x, f, out[:, 8:8 + f])
+    assert torch.all(out == 7.0)
+    y = out[:, 8:8 + 48]
+    gcnsa.op_layer_norm(x, f, y)
+    want = torch.nn.functional.layer_norm(x.double(), (f,), eps=1e-5)
+    # |xh| < sqrt(45) < 7; sums of 45 terms are off by at most 45 half units, of which rstd takes half, and six roundings beside
+    _within(y[:, :f], want, (22.5 + 6) * 2.0**-24 * 7, "y")
+    _pads_are_zero(y, f)
+    assert torch.all(out[:, :8] == 7.0) and torch.all(out[:, 56:] == 7.0)

@@ -121,3 +121,30 @@ def test_host_tensors_and_wrong_types_are_refused():
         with pytest.raises(gcnsa.GcnsaError):
             gcnsa.Packed8(*bad, device="cpu")
     assert p.q.shape == (4, 32) and p.e.shape == (4, 1) and gcnsa.Packed8(3, 33, device="cpu").q.shape == (3, 48)
+
+
+def test_dimensions_that_tiles_would_carry_past_32_bits_are_refused():
+    L, big = gcnsa.lib(), 2**31 - 2**17
+    for n, f in ((big, 128), (1, big)):
+        p = _p8(ldq=2**31, lde=2**26)
+        assert L.gcnsa_op_pack8(None, n, f, BASE, 2**31, p) == gcnsa.ERR_ARG
+        assert L.gcnsa_op_unpack8(None, n, f, p, BASE, 2**31) == gcnsa.ERR_ARG
+    for n, f, c in ((big, 8, 8), (8, big, 8), (8, 8, big)):
+        assert L.gcnsa_op_gemm_packed8(None, n, f, c, _p8(ldq=2**31, lde=2**26), BASE, 2**31, BASE, 2**31, 0, BASE, 1 << 50) == gcnsa.ERR_ARG
+    for n, d, c in ((big, 1, 1), (1, big, 1), (1, 1, big)):
+        assert L.gcnsa_op_linear_ce(None, n, d, c, BASE, 2**31, BASE + 16, 2**31, None, BASE, None, n, BASE, None, 0, None, 0, None, 0, BASE,
+                                    1 << 50) == gcnsa.ERR_TOO_LARGE
+
+
+def test_results_are_not_windows_whose_pad_columns_belong_to_others():
+    """A result's rows are written up to the next multiple of 4 columns: into the neighbours of a window, and past the last row's
+    end of memory."""
+    big = torch.zeros(5, 24)
+    for cols, view in ((9, big[:, :9]), (9, big[:, 3:12]), (21, big[:, 3:])):
+        assert gcnsa._matrix(view, "x", "float32", 5, cols, -1)[1] == 24          # as an input: fine
+        with pytest.raises(gcnsa.GcnsaError) as e:
+            gcnsa._matrix(view, "y", "float32", 5, cols, -1, True)
+        assert e.value.code == gcnsa.ERR_ARG
+    for cols, view in ((9, big[:, :12]), (12, big[:, :12]), (24, big), (8, big[:, 16:]), (9, torch.zeros(5, 9))):
+        assert gcnsa._matrix(view, "y", "float32", 5, cols, -1, True)[1] == view.stride(0)
+    assert gcnsa._matrix(big[:1, :9], "y", "float32", 1, 9, -1, True)[1] == 9      # a single row ends with its window
