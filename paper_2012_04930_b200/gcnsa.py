@@ -753,16 +753,17 @@ def _refuse(what):
 
 
 _torch_api = None
+_dtypes = {}
 
 
 def _torch():
-    """(torch, its dtypes by name, raw stream of a device, current device): looked up once, as these calls cost more host time
-    than the launches of a small operator."""
+    """(raw stream of a device, current device), and the dtypes by name: looked up once, as the checks cost more host time
+    than the launches of a small operator (so they ask a tensor as few questions as they can, too)."""
     global _torch_api
     if _torch_api is None:
         import torch
-        dtypes = {n: getattr(torch, n) for n in ("float32", "int32", "int8", "uint8")}
-        _torch_api = (torch, dtypes, torch._C._cuda_getCurrentRawStream, torch.cuda.current_device)
+        _dtypes.update((n, getattr(torch, n)) for n in ("float32", "int32", "int8", "uint8"))
+        _torch_api = (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
     return _torch_api
 
 
@@ -770,7 +771,9 @@ def _vector(t, name, dtype, size, dev):
     """Pointer of a contiguous device vector of at least `size` elements, or None."""
     if t is None:
         return None
-    if t.get_device() != dev or t.dtype is not _torch()[1][dtype] or not t.is_contiguous() or t.numel() < size:
+    if not _dtypes:
+        _torch()
+    if t.get_device() != dev or t.dtype is not _dtypes[dtype] or not t.is_contiguous() or t.numel() < size:
         _refuse(f"{name}: a contiguous {dtype} vector of {size} elements on cuda:{dev} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -781,15 +784,21 @@ def _matrix(t, name, dtype, rows, cols, dev, result=False):
     be the tensor's own."""
     if t is None:
         return None, 0
+    if not _dtypes:
+        _torch()
     shape = t.shape
-    if (len(shape) != 2 or shape[0] != rows or shape[1] < cols or t.get_device() != dev or t.dtype is not _torch()[1][dtype] or
-            (shape[1] > 1 and t.stride(1) != 1)):
+    if len(shape) != 2:
+        _refuse(f"{name}: a matrix is needed, got {tuple(shape)}")
+    r, c = shape
+    ld, step = t.stride()
+    if r != rows or c < cols or t.get_device() != dev or t.dtype is not _dtypes[dtype] or (step != 1 and c > 1):
         _refuse(f"{name}: rows of contiguous {dtype} columns on cuda:{dev} are needed, [{rows} x at least {cols}], got {t.dtype} "
-                f"{tuple(shape)} with strides {t.stride() if t.dim() else ()} on {t.device}")
-    if result and rows > 1 and shape[1] < min(t.stride(0), (cols + 3) // 4 * 4):
-        _refuse(f"{name}: a window of {shape[1]} columns in rows of {t.stride(0)}; columns up to {(cols + 3) // 4 * 4} are written (zeros behind {cols})")
-    # (the stride of a single row says nothing)
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(shape[1], cols)
+                f"{tuple(shape)} with strides {t.stride()} on {t.device}")
+    if rows <= 1:  # (the stride of a single row says nothing)
+        return t.data_ptr(), c
+    if result and c < ld and c < (cols + 3) // 4 * 4:
+        _refuse(f"{name}: a window of {c} columns in rows of {ld}; columns up to {min(ld, (cols + 3) // 4 * 4)} are written (zeros behind {cols})")
+    return t.data_ptr(), ld
 
 
 def _bytes_of(t, name, dev):
@@ -803,15 +812,16 @@ def _bytes_of(t, name, dev):
 
 def _leader(t, name):
     """(rows, device index, stream) of the matrix whose device the call goes to; that device has to be the current one."""
-    if t is None or t.dim() != 2:
+    shape = () if t is None else t.shape
+    if len(shape) != 2:
         _refuse(f"{name}: a matrix is needed")
     dev = t.get_device()
     if dev < 0:
         _refuse(f"{name}: on {t.device}, a CUDA device is needed")
-    _, _, raw_stream, current = _torch()
+    raw_stream, current = _torch_api or _torch()
     if dev != current():
         _refuse(f"{name}: on cuda:{dev}, the current device is cuda:{current()}")
-    return t.shape[0], dev, raw_stream(dev)
+    return shape[0], dev, raw_stream(dev)
 
 
 class Packed8:
