@@ -246,10 +246,13 @@ __device__ __forceinline__ void load_cols(const float* __restrict__ w, float non
 // one: a column offset of 1e4 next to a spread of 1 then costs no digits, as the differences x - mean are exact.
 //
 // A short row is the chain load - two sums across lanes - store: a warp that holds few float4 of a row works on R at a time
-// (200 000 x 100: 66 us with one, 56 with four).  The rest is registers, for enough warps: 83 194 x 601 takes 147 us with 172 a
+// (200 000 x 100: 66 us with one, 56 with four); two rows share a block's barriers (33 333 x 1 500: 121 and 109; by 4-byte
+// accesses two cost registers, 168 and 187 for 48 543 x 1 030).  The rest is registers, for enough warps: 83 194 x 601 takes 147 us with 172 a
 // thread, 94 with 128 and a few spilled; 48 543 x 1 030 by 4-byte accesses 433 with 148, 168 with 64.  The grid is what the SMs
 // hold at once (twice as many blocks: 83 194 x 601 96, 50 003 x 1 001 72 for 70).
-GCNSA_HD constexpr int norm_rows_at_once(int t, int nv) { return t > 32 ? 1 : t < 32 ? 2 : nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+GCNSA_HD constexpr int norm_rows_at_once(int t, int nv, bool vec) {
+  return t > 32 ? (vec && nv == 2 ? 2 : 1) : t < 32 ? 2 : nv == 1 ? 4 : nv == 2 ? 2 : 1;
+}
 constexpr int norm_blocks_per_sm(int t, int nv) { return nv <= 2 ? 4 : t <= 32 && nv <= 4 ? 3 : 2; }
 template <int T, int NV, bool VEC>
 __global__ void __launch_bounds__(kNormThreads, norm_blocks_per_sm(T, NV))
@@ -257,7 +260,7 @@ layer_norm_rows(int64_t n, int f, const float* x, int64_t ldx, const float* __re
                 float eps, int relu, float* y, int64_t ldy, float* __restrict__ mean_out, float* __restrict__ rstd_out,
                 PackedRows x8, PackedRows y8, BitRows bits) {
   wait_for_predecessors();
-  constexpr int R = norm_rows_at_once(T, NV), TEAMS = kNormThreads / T;
+  constexpr int R = norm_rows_at_once(T, NV, VEC), TEAMS = kNormThreads / T;
   __shared__ float sh1[2][R][kNormThreads / 32], sh2[2][2 * R][kNormThreads / 32];
   const int t = threadIdx.x % T, team = threadIdx.x / T;
   const int n_pad = (int)min(ldy, (int64_t)((f + 3) / 4 * 4));
@@ -772,7 +775,7 @@ int launch_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_
     run(layer_norm_wide, row_blocks(n, 1, 148 * 8));
   } else {
     const RowTeam m = row_team(f, kNormLaneVecs);
-    const int blocks = row_blocks(n, kNormThreads / m.t * norm_rows_at_once(m.t, m.nv), 148 * norm_blocks_per_sm(m.t, m.nv));
+    const int blocks = row_blocks(n, kNormThreads / m.t * norm_rows_at_once(m.t, m.nv, vec), 148 * norm_blocks_per_sm(m.t, m.nv));
 #define GCNSA_NORM(T, NV) (vec ? run(layer_norm_rows<T, NV, true>, blocks) : run(layer_norm_rows<T, NV, false>, blocks))
     if (m.t == 8) GCNSA_NORM(8, 1);
     else if (m.t == 16) GCNSA_NORM(16, 1);
