@@ -182,10 +182,12 @@ __global__ void __launch_bounds__(256) loss_total(int n, const LossSum* __restri
   wait_for_predecessors();
   finish_loss(n, sums, total, n_train, loss);
 }
-// logsumexp of every row from the runs that crossed its tile, and a block's sum of losses
+// Maximum and 1 / sum of exponentials of every row from the runs that crossed its tile, and a block's sum of losses.  The two are
+// kept apart: as one number, the maximum plus the sum's logarithm, they would be off by half a unit of the maximum, which a
+// probability near 1 has above its distance from 1 (logits near 1 000: 3e-5 of p - 1).
 __global__ void __launch_bounds__(256)
 row_finish(int64_t rows, int c, int tiles_n, int total, int grid, const float* __restrict__ part_m, const float* __restrict__ part_s,
-           const int32_t* __restrict__ y, const float* __restrict__ zy, float* __restrict__ lse, LossSum* __restrict__ losses) {
+           const int32_t* __restrict__ y, const float* __restrict__ zy, float2* __restrict__ top, LossSum* __restrict__ losses) {
   wait_for_predecessors();
   __shared__ double sh[8];
   const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -198,14 +200,13 @@ row_finish(int64_t rows, int c, int tiles_n, int total, int grid, const float* _
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t slot = ((int64_t)(b + t) * 2 + h) * BM + r % BM;
-        const float pm = part_m[slot], top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
+        const float pm = part_m[slot], larger = fmaxf(m, pm), base = larger == -INFINITY ? 0.f : larger;
         s = s * expf(m - base) + part_s[slot] * expf(pm - base);
-        m = top;
+        m = larger;
       }
-    const float l = (m == -INFINITY ? 0.f : m) + logf(s);
     const int label = y[r];
-    lse[r] = l;
-    loss = label >= 0 && label < c ? l - zy[r] : NAN;  // (no class was a label outside)
+    top[r] = make_float2(m, 1.f / s);
+    loss = label >= 0 && label < c ? ((double)m - zy[r]) + logf(s) : NAN;  // (no class was a label outside)
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(kFull, loss, o);
@@ -283,7 +284,7 @@ constexpr int kWholeCols = 128;                    // classes that one tile hold
 constexpr int64_t kPieceFloats = int64_t(40) << 20;
 struct CePlan {
   int64_t gt_floats, partial_floats, sums_floats, slots;
-  size_t gt, partial, sums, hc, wc, yc, rows, place, counts, total, zy, lse, part, losses, end;
+  size_t gt, partial, sums, hc, wc, yc, rows, place, counts, total, zy, top, part, losses, end;
 };
 CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   CePlan p;
@@ -307,7 +308,7 @@ CePlan ce_plan(int64_t n, int32_t d, int32_t c) {
   p.counts = take((size_t)div_up(n, kRowsPerBlock) * 4);
   p.total = take(4);
   p.zy = take((size_t)n * 4);
-  p.lse = take((size_t)n * 4);
+  p.top = take((size_t)n * sizeof(float2));
   p.part = take((size_t)p.slots * 2 * BM * 2 * 4);
   p.losses = take((size_t)std::max<int64_t>(sms * kFoldWarps, div_up(n, 256)) * sizeof(LossSum));
   p.end = at;
@@ -462,9 +463,9 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     GCNSA_STEP((run_terms<TermShape<128, ASrc::kMajor, false, Out::stats>>(s, t, grid)));
     end.n = (int)div_up(R, 256);
     GCNSA_STEP(launch(row_finish, end.n, 256, 0, s, R, a.c, t.p[0].tiles_n, t.total, grid, (const float*)t.ce.part_m, (const float*)t.ce.part_s,
-                      y, (const float*)t.ce.zy, f_at(pl.lse), losses));
+                      y, (const float*)t.ce.zy, (float2*)(ws + pl.top), losses));
     note_launch(2);
-    t.ce.lse = f_at(pl.lse);
+    t.ce.top = (const float2*)(ws + pl.top);
   }
   if (!grads || R == 0 || (!a.dw && !a.db)) {  // no launch of add_slices to come
     GCNSA_STEP(launch(loss_total, 1, 256, 0, s, end.n, (const LossSum*)losses, total, a.n_train, a.loss));

@@ -77,7 +77,7 @@ struct CeTile {
   int c0, ldg;
   float inv_nt;
   float* gt;             // G^T: [class of the piece][ldg]; nullable (Out::whole)
-  const float* lse;      // [M] (Out::grad)
+  const float2* top;     // [M] maximum and 1 / sum of exponentials of a row (Out::grad)
   float *part_m, *part_s, *zy;  // (Out::stats) running maximum and sum of a CTA's run in a row tile, the label's logit
   LossSum* losses;       // (Out::whole) a sum per fold warp of the grid
 };
@@ -631,12 +631,12 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
       const bool row_in = m < p.M;
       // what the epilogue needs of its row, on the way while the sums are made
       int label = -1;
-      float lse = 0.f;
+      float2 top = {0.f, 0.f};
       bool on = row_in;
       if constexpr (S::OUT != Out::transposed) {
         if (row_in) label = max(__ldg(args.ce.y + m), -1);
         if constexpr (S::OUT == Out::grad)
-          if (row_in) lse = __ldg(args.ce.lse + m);
+          if (row_in) top = __ldg(args.ce.top + m);
         if constexpr (S::OUT == Out::whole) on = row_in && (!args.ce.mask || __ldg(args.ce.mask + m) != 0);
       }
       float sum[HALF];
@@ -727,18 +727,26 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
         const bool here = row_in && label >= 0 && label < cols;
         const bool any_here = __any_sync(0xffffffffu, here);  // (few of the tiles have a label of a warp's rows)
         if constexpr (S::OUT == Out::grad) {
-          const float scale = args.ce.inv_nt, shift = -lse;
+          const float scale = top.y * args.ce.inv_nt;
+          float own = 0.f;
 #pragma unroll
-          for (int j = 0; j < HALF; ++j) sum[j] = exp2_fast((sum[j] + shift) * kLog2e);
+          for (int j = 0; j < HALF; ++j) sum[j] = exp2_fast((sum[j] - top.x) * kLog2e);
           if (any_here)
 #pragma unroll
-            for (int j = 0; j < HALF; ++j) sum[j] -= j == label ? 1.f : 0.f;
+            for (int j = 0; j < HALF; ++j) own = j == label ? sum[j] : own;
+#pragma unroll
+          for (int j = 0; j < HALF; ++j) sum[j] *= scale;
+          if (any_here) {  // the label's: p is rounded once, with the 1 taken off
+            own = fmaf(own, top.y, -1.f) * args.ce.inv_nt;
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) sum[j] = j == label ? own : sum[j];
+          }
           if (row_in) {
             const int64_t ldg = args.ce.ldg;
             float* at = args.ce.gt + nb * ldg + m;
 #pragma unroll
             for (int j = 0; j < HALF; ++j, at += ldg)
-              if (j < cols) *at = sum[j] * scale;
+              if (j < cols) *at = sum[j];
           }
         } else {
           float mx = -INFINITY, zy = 0.f;

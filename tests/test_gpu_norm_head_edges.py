@@ -1,0 +1,78 @@
+"""GPU tests of layer norm, 8-bit checkpoints and output layers at the edges of what their calls allow: logits far from zero,
+classes and rows left out, values that are not finite, pad columns.  Bounds count half units u = 2^-24, as in
+test_gpu_norm_head.py."""
+import math
+
+import pytest
+import torch
+
+from paper_2012_04930_b200 import gcnsa
+from test_gpu_norm_head import U, _buf, _bytes, _ce_run, _empty, _rand, _within
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------ output layer ---
+def _exact_logits(c, offset):
+    """Logits that fp32 holds exactly (so do the products): a row of h picks a row of w, whose entries are multiples of 2^-10, and
+    the bias puts all of them `offset` off zero.  A class of every row of w stands 4 to 19 above the rest; four rows in five have
+    it as their label."""
+    n, d = 400, 16
+    h = torch.zeros(n, d, device="cuda")
+    k = torch.arange(n, device="cuda") % d
+    h[torch.arange(n), k] = 1
+    w = torch.round(_rand(c, d, c) * 1024) / 1024
+    top = torch.arange(d, device="cuda") * 37 % c
+    w[torch.arange(d), top] += 4 + torch.arange(d, device="cuda")
+    y = top[k]
+    y[::5] = (y[::5] + 1) % c
+    return h, w, torch.full((c,), float(offset), device="cuda"), y.int()
+
+
+def _exact_logits64(h, w, bias, y):
+    """Loss and gradients in 64 bits and bounds for exact logits.  x = z - max is exact; x log2(e) is off by 2 u (the constant, the
+    product), so its exponential by 2 u |x|, and ex2 by 4 u; a maximum that moves from tile to tile costs 5 u each; a sum has c / 32
+    + 24 additions in a row; 1 / sum, probability, label, share: a u each.  Where the offset lies enters none of it."""
+    n, c = h.shape[0], w.shape[1]
+    z = h.double() @ w.double() + bias.double()
+    x = z - z.max(1, keepdim=True).values
+    p = torch.softmax(z, 1)
+    far = torch.where(p > 0, p * x.abs(), torch.zeros_like(p))          # (0 for a class at -infinity)
+    label = torch.nn.functional.one_hot(y.long(), c).double()
+    G = (p - label) / n
+    es = U * ((2 * far).sum(1) + 5 * ((c + 127) // 128 + 2) + c / 32 + 24)
+    eG = (2 * U * far + p * (6 * U + es[:, None]) + 4 * U * (p - label).abs()) / n + 1e-37
+    row = -torch.log_softmax(z, 1).gather(1, y.long()[:, None])[:, 0]
+    log_s = torch.log(torch.exp(x).sum(1))
+    ht, wt = h.double().abs(), w.double().abs()
+    return {"loss": (row.mean(), (es + 4 * U * (row + log_s)).mean()),
+            "dh": (G @ w.double().t(), eG @ wt.t() + (c + 16) * U * (G.abs() @ wt.t())),
+            "dw": (h.double().t() @ G, ht.t() @ eG + (n + 16) * U * (ht.t() @ G.abs())),
+            "db": (G.sum(0), eG.sum(0) + (n + 16) * U * G.abs().sum(0))}
+
+
+@pytest.mark.parametrize("offset", [0, 30, 1000, -8000])
+@pytest.mark.parametrize("c", [129, 700])
+def test_confident_rows_far_from_zero(c, offset):
+    """p - 1 of a confident row is what is left of two nearly equal numbers: maximum and sum of a row are kept apart, as
+    their logarithm in one number would be off by half a unit of the offset."""
+    h, w, bias, y = _exact_logits(c, offset)
+    want = _exact_logits64(h, w, bias, y)
+    got = _ce_run(h, w, bias, y, None, h.shape[0])
+    for k in want:
+        _within(got[k], *want[k], f"{k} c={c} offset={offset}")
+
+
+@pytest.mark.parametrize("left_out", [torch.finfo(torch.float32).min, -math.inf])
+@pytest.mark.parametrize("c", [41, 128, 129, 700])
+def test_a_class_left_out_by_its_bias(c, left_out):
+    h, w, bias, y = _exact_logits(c, 4)
+    out = (int(y.max()) + 5) % c
+    while bool((y == out).any()):
+        out = (out + 1) % c
+    bias[out] = left_out
+    want = _exact_logits64(h, w, bias, y)
+    got = _ce_run(h, w, bias, y, None, h.shape[0])
+    for k in ("loss", "dh", "dw", "db"):
+        _within(got[k], *want[k], f"{k} c={c}")
+    assert torch.all(got["dw"][:, out] == 0) and got["db"][out] == 0
