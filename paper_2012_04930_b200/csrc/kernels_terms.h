@@ -795,7 +795,8 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
             if (row_in) {
               const float inv = 1.f / s;
               // the half that has the label's logit adds the row's loss (a label outside all classes: no loss is a number)
-              if (on && here) mine.loss += (base + logf(s)) - zy;
+              // (its distance from the maximum first: log(s) added to a large maximum would lose its digits)
+              if (on && here) mine.loss += (base - zy) + logf(s);
               if (on && half == 0) {
                 if (label + c0 < 0 || label + c0 >= p.N) mine.loss = NAN;
                 ++mine.count;

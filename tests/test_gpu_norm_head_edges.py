@@ -76,3 +76,14 @@ def test_a_class_left_out_by_its_bias(c, left_out):
     for k in ("loss", "dh", "dw", "db"):
         _within(got[k], *want[k], f"{k} c={c}")
     assert torch.all(got["dw"][:, out] == 0) and got["db"][out] == 0
+
+
+@pytest.mark.parametrize("offset", [0, 30, 1000, -8000])
+@pytest.mark.parametrize("c", [2, 41, 64, 128])
+def test_confident_rows_of_a_few_classes(c, offset):
+    """The same where a tile holds whole rows: the label's distance from the maximum is taken before the sum's logarithm is added."""
+    h, w, bias, y = _exact_logits(c, offset)
+    want = _exact_logits64(h, w, bias, y)
+    got = _ce_run(h, w, bias, y, None, h.shape[0])
+    for k in want:
+        _within(got[k], *want[k], f"{k} c={c} offset={offset}")
