@@ -694,6 +694,8 @@ size_t gcnsa_op_gemm_packed8_workspace(int64_t n, int32_t f, int32_t c);
  * masked rows (n without a mask); with another number the loss comes out as NaN.
  * n_train = 0: loss 0, zero gradients.  Labels of masked rows lie in [0, c); one
  * that does not makes the loss NaN (nothing is read or written out of place).
+ * Rows that do not count (mask 0) may hold anything in h and y: their dh is 0 and
+ * nothing else depends on them.
  * accumulate applies to dw and db.  d, c >= 1; n, d, c < 2^31 - 2^17, n c < 2^45; workspace: DEVICE,
  * 256-byte aligned, gcnsa_op_linear_ce_workspace(n, d, c) bytes. */
 int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const float* h, int64_t ldh, const float* w,

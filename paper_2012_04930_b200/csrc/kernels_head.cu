@@ -9,6 +9,7 @@
 //  - c > 128: one pass keeps a running maximum and sum of exponentials per row (8 bytes per row and run of tiles), then, a
 //    piece of the classes at a time, z is made again and turned into G.  Rows that
 //    do not count are left out of all products: the others are gathered first.
+// Rows that do not count may hold anything: up to 128 classes they are rows of zeros in G, and in H^T G rows of zeros of H too.
 // The two gradient products of a piece are independent and run as one launch, the slices of dW^T before the tiles of dH^T.
 #include <cuda_runtime.h>
 
@@ -514,6 +515,7 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
       pw.accumulate = split ? 0 : a.accumulate;
       pw.m_pad = (int)(split ? up4(width) : dw_pad);
       pw.k_rows = R;
+      pw.k_mask = whole ? a.mask : nullptr;  // (rows that do not count are still there: 0 in G, but 0 x NaN is NaN)
       if (a.db) {
         pw.a_sums = f_at(pl.sums);
         pw.sums_pitch = up4(width);

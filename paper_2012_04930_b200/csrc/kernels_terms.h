@@ -60,6 +60,7 @@ struct Product {
   int write;               // 0: only a_sums are wanted
   const float* a;          // ASrc::direct
   int64_t lda, k_rows;
+  const uint8_t* k_mask;   // nullable [k_rows], B as floats: lines of B whose byte is 0 count as zeros, whatever they hold
   const uint8_t* e;        // steps of a packed B
   int64_t lde;
   int e_blocks;
@@ -262,6 +263,12 @@ struct TermB {  // a lane has four neighbouring n of line(i), i below COUNT
     const int n = 4 * (lane % LANES);
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) x[i] = *reinterpret_cast<const float4*>(raw + (n / 32) * 4096 + line(i, wq, lane) * 128 + (n & 31) * 4);
+  }
+  // zeros for the lines wq * 8 + k with bit k of `lines`
+  __device__ __forceinline__ void clear(uint32_t lines, int lane) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+      if ((lines >> line(i, 0, lane)) & 1u) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   __device__ __forceinline__ void store(uint8_t* terms, int wq, int lane, uint32_t) const {
     const int n = 4 * (lane % LANES);
@@ -580,8 +587,16 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
       const uint8_t* const e_at = p.e + (p.k_rows - k_left) * lde + wk.n0 / 32 + lane % EB;
       const bool e_in = S::P8 && lane < 8 * EB && wk.n0 / 32 + lane % EB < p.e_blocks;
       auto step_of = [&](int it) { return e_in && it < wk.n_kb && it * BK < k_left ? __ldg(e_at + (int64_t)it * BK * lde) : 0u; };
+      // lines of B that do not count: a lane has the byte of line q * 8 + lane % 8, fetched one k-block (of this group) ahead
+      constexpr bool MASKED = !S::P8 && S::OUT == Out::transposed;
+      const uint8_t* const k_mask = MASKED ? p.k_mask : nullptr;
+      auto counts = [&](int it) {
+        const int64_t k = (int64_t)(wk.kb0 + it) * BK + q * 8 + (lane & 7);
+        return !k_mask || it >= wk.n_kb || k >= p.k_rows ? 1u : (uint32_t)__ldg(k_mask + k);
+      };
       int it = (int)((group + S::BG - g % S::BG) % S::BG);
       g += it;
+      uint32_t counts_next = MASKED ? counts(it) : 1u;
       uint32_t e_next[3];
 #pragma unroll
       for (int i = 0; i < 3; ++i) e_next[i] = step_of(it + i * S::BG);
@@ -590,10 +605,14 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
         e_next[0] = e_next[1];
         e_next[1] = e_next[2];
         e_next[2] = step_of(it + 3 * S::BG);
+        const uint32_t left_out = MASKED ? __ballot_sync(0xffffffffu, counts_next == 0) & 0xffu : 0u;
+        if constexpr (MASKED) counts_next = counts(it + S::BG);
         ok = __all_sync(0xffffffffu, mbar_wait_long(&full_b[g % NB], (g / NB) & 1, 44));
         if (!ok) break;
         TermB<S> tb;
         tb.load(smem + S::B_OFF + (g % NB) * S::B_SLOT, q, lane);
+        if constexpr (MASKED)
+          if (left_out) tb.clear(left_out, lane);
         if (g >= NSB) ok = __all_sync(0xffffffffu, mbar_wait(&retired[(g - NSB) % kRetired], ((g - NSB) / kRetired) & 1, 45));
         if (!ok) break;
         tb.store(smem + S::T_OFF + sb * NTB * S::B_TERM, q, lane, e8);

@@ -87,3 +87,23 @@ def test_confident_rows_of_a_few_classes(c, offset):
     got = _ce_run(h, w, bias, y, None, h.shape[0])
     for k in want:
         _within(got[k], *want[k], f"{k} c={c} offset={offset}")
+
+
+@pytest.mark.parametrize("padded", [True, False])
+@pytest.mark.parametrize("c", [1, 41, 64, 128, 129, 700])
+def test_rows_that_do_not_count_may_hold_anything(c, padded):
+    n, d = 1111, 45
+    h, w, y = _rand(1, n, d), _rand(2, d, c) / 7, torch.arange(n, device="cuda", dtype=torch.int32) % c
+    mask = (_rand(3, n) < 0.5).to(torch.uint8)
+    mask[200:330] = 0                                  # whole blocks of rows among them
+    off = torch.nonzero(mask == 0)[:, 0]
+    nt = int(mask.sum())
+    h[off] = 0
+    want = _ce_run(h, w, None, y, mask, nt, padded)
+    assert all(torch.isfinite(v).all() for v in want.values())
+    for bad in (math.nan, math.inf, -math.inf, 3e38):
+        h[off] = bad
+        got = _ce_run(h, w, None, y, mask, nt, padded)
+        for k in want:
+            assert torch.equal(got[k], want[k]), (k, bad)
+    assert torch.all(got["dh"][off] == 0)
