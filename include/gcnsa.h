@@ -624,7 +624,7 @@ int gcnsa_op_colsum_static(void* stream, int64_t n, int32_t f, const float* g, i
  * a loss whose logits are never stored.  Results whose leading dimension leaves
  * room have zeros in the pad columns up to the next multiple of 4, in the last
  * row too (so a result is not a window of a wider matrix unless the pad columns
- * belong to it).  A workspace or scratch is in use until the kernels of its call
+ * belong to it); where a call adds to a result (accumulate), these stay as they are.  A workspace or scratch is in use until the kernels of its call
  * have run: calls (and captured graphs) that may run at the same time need one
  * each. */
 

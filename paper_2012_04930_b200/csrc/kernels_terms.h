@@ -54,7 +54,7 @@ struct Product {
   float* c;                // element (m, n) at c[z * slice_stride + row(n) * ldc + m]
   int64_t ldc, slice_stride;
   const int32_t* row_map;  // row(n), nullable; negative: not written
-  int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros
+  int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros (left as they are with accumulate)
   float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(AG z + g) * sums_pitch + m]
   int64_t sums_pitch;
   int write;               // 0: only a_sums are wanted
@@ -689,14 +689,17 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
       }
       if (!ok) break;
       if constexpr (S::OUT == Out::transposed) {
-        if (p.write && m < p.m_pad) {
+        const bool add = p.accumulate != 0;
+        if (p.write && m < (add ? p.M : p.m_pad)) {
+          if (!row_in)  // (not the accumulator: 0 x NaN where B has one)
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) sum[j] = 0.f;
           // (with what is there added) 8 lines at a time: where they go, what is there, then the stores (one by one every load would wait for the store
           // before it, as the compiler cannot tell that the lines differ)
           float* const dst = p.c + wk.z * p.slice_stride + m;
           const int32_t* const row_map = p.row_map;
           const int64_t ldc = p.ldc;
           const int left = p.N - nb;
-          const bool add = p.accumulate != 0;
           if (!row_map && !add) {
             float* at = dst + nb * ldc;
 #pragma unroll

@@ -107,3 +107,31 @@ def test_rows_that_do_not_count_may_hold_anything(c, padded):
         for k in want:
             assert torch.equal(got[k], want[k]), (k, bad)
     assert torch.all(got["dh"][off] == 0)
+
+
+# ------------------------------------------------------------- pad columns ---
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("n", [30, 5000])
+def test_pad_columns_beside_values_that_are_not_finite(n, accumulate):
+    """A line of a result has zeros up to the next multiple of 4 (with accumulate: what was there), whatever the products hold and
+    however many slices they are cut into."""
+    pad = 7.0 if accumulate else 0.0
+    f, c = 40, 5
+    p = gcnsa.Packed8(n, f)
+    x = _rand(1, n, f)
+    x[n // 2, 3] = math.nan
+    gcnsa.op_pack8(x, p)
+    dw = torch.full((f, 16), 7.0, device="cuda")
+    gcnsa.op_gemm_packed8(p, _rand(2, n, 16), c, dw, accumulate=accumulate, workspace=_bytes(gcnsa.op_gemm_packed8_workspace(n, f, c)))
+    assert torch.isnan(dw[:32, :c]).all() and torch.isfinite(dw[32:, :c]).all()
+    assert torch.all(dw[:, c:8] == pad) and torch.all(dw[:, 8:] == 7.0)
+    for c in (5, 131):
+        d = 6
+        h, w, y = _rand(3, n, 16), _rand(4, d, 144), torch.zeros(n, dtype=torch.int32, device="cuda")
+        h[n // 3, 2] = math.nan
+        loss, dh, dw = torch.empty(1, device="cuda"), torch.full((n, 16), 7.0, device="cuda"), torch.full((d, 144), 7.0, device="cuda")
+        gcnsa.op_linear_ce(h, d, w, c, y, n, loss, dh=dh, dw=dw, accumulate=accumulate, workspace=_bytes(gcnsa.op_linear_ce_workspace(n, d, c)))
+        assert torch.isnan(loss).all() and torch.isnan(dh[n // 3, :d]).all() and torch.isnan(dw[:, :c]).all()
+        up = (c + 3) // 4 * 4
+        assert torch.all(dw[:, c:up] == pad) and torch.all(dw[:, up:] == 7.0), c
+        assert torch.all(dh[:, d:8] == 0) and torch.all(dh[:, 8:] == 7.0), c
