@@ -400,7 +400,11 @@ layer_norm_grad(int64_t n, int f, const float* g, int64_t ldg, const float* x, i
             if (near_zero(fmaf((a[i] - mu) * r, ga[i], be[i]), be[i]) && !exactly_positive(a[i], mu, r, ga[i], be[i])) u[i] = 0.f;
       }
     }
-    // (columns past the end: u is 0, and what xh is there enters nothing that is written)
+    // Columns past the end: u is 0, and what xh is there enters nothing that is written, as long as it is finite.  (It is -mu r in all
+    // of them; a select per value instead of this question per row costs 4 to 7 % at 1 030 columns.)
+    if (isinf(mu * r))
+#pragma unroll
+      for (int i = 0; i < 4 * NV; ++i) a[i] = col_of<T, VEC>(i / 4, i % 4, t) < f ? a[i] : mu;
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4 * NV; ++i) {

@@ -135,3 +135,26 @@ def test_pad_columns_beside_values_that_are_not_finite(n, accumulate):
         up = (c + 3) // 4 * 4
         assert torch.all(dw[:, c:up] == pad) and torch.all(dw[:, up:] == 7.0), c
         assert torch.all(dh[:, d:8] == 0) and torch.all(dh[:, 8:] == 7.0), c
+
+
+# -------------------------------------------------------------- layer norm ---
+@pytest.mark.parametrize("f", [7, 9, 33, 100, 130, 300, 600, 1001, 1500, 4100, 8200])
+def test_norm_backward_of_equal_values_far_from_zero(f):
+    """x is its own mean: xh is 0 and dx = rstd (u - mean(u)).  The places of a team past the row's end have no say, though there
+    (0 - mean) rstd is beyond fp32."""
+    n = 9
+    x, mean, rstd = torch.full((n, f), 2.0 ** 123, device="cuda"), torch.full((n,), 2.0 ** 123, device="cuda"), torch.full((n,), 316.0, device="cuda")
+    g, gamma = _rand(f, n, f), _rand(f + 1, f)
+    p = gcnsa.Packed8(n, f)
+    gcnsa.op_pack8(x, p)                                # (a power of two: the checkpoint holds it as it is)
+    u = g.double() * gamma.double()
+    want = 316.0 * (u - u.mean(1, keepdim=True))
+    bound = (max(32, f / 256) + 25) * U * 316.0 * (u.abs() + u.abs().mean(1, keepdim=True))
+    for padded in (True, False):
+        for src in (_buf(x, padded), p):
+            for relu, beta in ((0, None), (1, torch.ones(f, device="cuda"))):   # (v = 1: the ReLU lets all through)
+                dx, dg = _empty(n, f, padded), torch.empty(f, device="cuda")
+                gcnsa.op_layer_norm_backward(_buf(g, padded), src, f, dx, mean, rstd, gamma=gamma, beta=beta, relu=relu, dgamma=dg,
+                                             scratch=_bytes(gcnsa.op_layer_norm_backward_scratch(n, f)))
+                _within(dx[:, :f], want, bound, f"dx f={f}")
+                assert torch.all(dg == 0)
