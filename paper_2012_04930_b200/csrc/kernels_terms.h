@@ -27,10 +27,12 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "launch.h"
 #include "pack8_device.h"
+#include "register_split.h"
 #include "tc_device.h"
 #include "tma_host.h"
 
@@ -189,9 +191,11 @@ struct TermShape {
   static constexpr int AG = P8 ? 3 : 2, BG = 2;          // groups of four warps that make terms of A, of B
   static constexpr int BWARP0 = kAWarp0 + 4 * AG, FWARP0 = BWARP0 + 4 * BG, THREADS = 32 * (FWARP0 + kFoldWarps);
   // registers per thread by role, in multiples of 8; their sum over the warpgroups is at most what the launch gives
-  static constexpr int REGS = P8 ? 64 : 72;              // (the compiler's, with that many threads)
+  static constexpr int REGS = P8 ? 64 : 72;              // (the compiler's, with that many threads; run_terms asks)
   static constexpr int REGS_ISSUE = P8 ? 24 : 32, REGS_A = 72, REGS_B = P8 ? 48 : 64, REGS_FOLD = P8 ? 88 : 96;
-  static_assert(REGS_ISSUE + AG * REGS_A + BG * REGS_B + 2 * REGS_FOLD <= THREADS / 128 * REGS, "setmaxnreg draws on the registers of the launch");
+  static constexpr bool A_INC = REGS_A > REGS;
+  static constexpr RegisterShare SHARES[4] = {{1, REGS_ISSUE, false}, {AG, REGS_A, A_INC}, {BG, REGS_B, false}, {kFoldWarps / 4, REGS_FOLD, true}};
+  static_assert(registers_hold(REGS, SHARES), "setmaxnreg draws on the registers of the launch");
   static constexpr int HALF = BN / 2;                    // columns of a fold warp
   // With one term of B all three products of a k-block share an accumulator, which is folded twice as often; the columns of
   // the third one hold more stages of A.
@@ -498,7 +502,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
     }
   } else if (warp < S::BWARP0) {
     // ---------------- terms of A: every AG-th k-block to a group ----------------
-    if constexpr (S::REGS_A > S::REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::REGS_A));
+    if constexpr (S::A_INC) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::REGS_A));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::REGS_A));
     const int q = warp & 3, group = (warp - kAWarp0) >> 2, row = 32 * q + lane;  // row of the tile
     uint32_t g = 0;
@@ -867,9 +871,24 @@ inline bool term_map(CUtensorMap* map, const void* base, bool bytes, int64_t out
             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Whether the compiled kernel has the registers that its warps divide (asked once).
+template <class S>
+cudaError_t registers_given() {
+  static std::atomic<bool> held{false};
+  if (held.load(std::memory_order_relaxed)) return cudaSuccess;
+  cudaFuncAttributes f;
+  const cudaError_t e = cudaFuncGetAttributes(&f, term_product<S>);
+  if (e != cudaSuccess) return e;
+  if (!registers_hold(f.numRegs, S::SHARES)) return cudaErrorInvalidKernelImage;
+  held.store(true, std::memory_order_relaxed);
+  return cudaSuccess;
+}
+
 template <class S>
 cudaError_t run_terms(cudaStream_t s, const TermArgs& a, int grid) {
-  cudaError_t e = cudaFuncSetAttribute(term_product<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM_BYTES);
+  cudaError_t e = registers_given<S>();
+  if (e != cudaSuccess) return e;
+  e = cudaFuncSetAttribute(term_product<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM_BYTES);
   if (e != cudaSuccess) return e;
   return launch(term_product<S>, grid, S::THREADS, S::SMEM_BYTES, s, a);
 }
