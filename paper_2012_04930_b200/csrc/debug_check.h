@@ -19,6 +19,8 @@ constexpr int kDbgLossColWrite = 6;  // transposed CSR over the loss columns: a 
 constexpr int kDbgPlanSlot = 7;      // plan of the tensor-core products: a row or column slot outside its tile's chunks
 constexpr int kDbgPlanRest = 8;      // plan: a write position outside the row's part of the remainder
 constexpr int kDbgPartialSum = 9;    // planned product: a partial sum outside the workspace
+constexpr int kDbgGatherPlace = 10;  // output layer: the place of a counted row outside the gathered rows
+constexpr int kDbgResultRow = 11;    // output layer: the row of a gathered row's gradient outside the matrix
 
 // Bounds a caller knows about the operands of one sparse product; -1 = not known, not checked.
 struct SpmmBounds {
@@ -45,5 +47,6 @@ __device__ __forceinline__ bool dbg_in(unsigned long long* word, long long v, lo
 int debug_word_spmm(unsigned long long* out, bool clear);
 int debug_word_build(unsigned long long* out, bool clear);
 int debug_word_dense(unsigned long long* out, bool clear);
+int debug_word_head(unsigned long long* out, bool clear);
 
 }  // namespace gcnsa

@@ -15,6 +15,7 @@
 
 #include <algorithm>
 
+#include "debug_check.h"
 #include "internal.h"
 #include "kernels_terms.h"
 #include "launch.h"
@@ -135,6 +136,9 @@ gather_rows(int64_t n, int d, const float* __restrict__ h, int64_t ldh, const in
   for (int64_t i = (int64_t)blockIdx.x * 8 + w; i < n; i += (int64_t)gridDim.x * 8) {
     const int at = place[i];
     if (at >= 0) {
+#if GCNSA_DBG
+      if (!dbg_in(&g_dbg_head, at, 0, room, kDbgGatherPlace)) continue;
+#endif
       const float* src = h + i * ldh;
       float* dst = hc + at * ldc;
       const int d4 = vec ? d / 4 : 0;
@@ -532,6 +536,7 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
       ph.c = a.dh;
       ph.ldc = a.lddh;
       ph.row_map = rows;
+      ph.map_rows = a.n;
       ph.accumulate = c0 > 0;
       ph.m_pad = (int)std::min<int64_t>(a.lddh, up4(a.d));
       ph.k_rows = width;
@@ -547,6 +552,21 @@ int launch_linear_ce(void* stream, const LinearCe& a, void* workspace) {
     }
   }
   return 0;
+}
+
+int debug_word_head(unsigned long long* out, bool clear) {
+  *out = 0ull;
+#if GCNSA_DBG
+  cudaError_t e = cudaMemcpyFromSymbol(out, g_dbg_head, sizeof(*out));
+  if (e == cudaSuccess && clear) {
+    const unsigned long long zero = 0ull;
+    e = cudaMemcpyToSymbol(g_dbg_head, &zero, sizeof(zero));
+  }
+  return (int)e;
+#else
+  (void)clear;
+  return 0;
+#endif
 }
 
 int tc_status_head(int* out) {

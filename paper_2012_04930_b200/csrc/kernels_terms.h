@@ -30,6 +30,7 @@
 #include <atomic>
 #include <cstdint>
 
+#include "debug_check.h"
 #include "launch.h"
 #include "pack8_device.h"
 #include "register_split.h"
@@ -38,6 +39,10 @@
 
 namespace gcnsa {
 namespace {
+
+#if GCNSA_DBG
+GCNSA_DBG_WORD(g_dbg_head);
+#endif
 
 constexpr int BM = 128, BK = 32;
 constexpr int kAWarp0 = 4, kFoldWarps = 8;
@@ -56,6 +61,7 @@ struct Product {
   float* c;                // element (m, n) at c[z * slice_stride + row(n) * ldc + m]
   int64_t ldc, slice_stride;
   const int32_t* row_map;  // row(n), nullable; negative: not written
+  int64_t map_rows;        // rows that row_map leads to
   int accumulate, m_pad;   // columns [M, m_pad) of a line are written as zeros (left as they are with accumulate)
   float* a_sums;           // nullable: sums of A's rows (over k) of slice z, k-blocks of group g: a_sums[(AG z + g) * sums_pitch + m]
   int64_t sums_pitch;
@@ -716,6 +722,12 @@ __global__ void __launch_bounds__(S::THREADS, 1) term_product(const __grid_const
               int r[8];
 #pragma unroll
               for (int j = 0; j < 8; ++j) r[j] = j0 + j >= left ? -1 : row_map ? __ldg(row_map + nb + j0 + j) : nb + j0 + j;
+#if GCNSA_DBG
+              if (row_map)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (r[j] >= 0 && !dbg_in(&g_dbg_head, r[j], 0, p.map_rows, kDbgResultRow)) r[j] = -1;
+#endif
               if (add) {
                 float was[8];
 #pragma unroll
