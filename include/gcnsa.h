@@ -679,7 +679,8 @@ int gcnsa_op_unpack8(void* stream, int64_t n, int32_t f, const gcnsa_packed8* p,
 
 /* dw (+)= X^T G with X [n x f] a checkpoint and G [n x c]: the weight gradient of a
  * layer whose input was kept in 8 bits.  fp32-level accuracy with respect to the
- * values the checkpoint stands for.  n, f, c < 2^31 - 2^17; workspace: DEVICE, 256-byte
+ * values the checkpoint stands for; a column of G with an infinity or a NaN gives
+ * NaN, not infinities.  n, f, c < 2^31 - 2^17; workspace: DEVICE, 256-byte
  * aligned, gcnsa_op_gemm_packed8_workspace(n, f, c) bytes (NULL when that is 0). */
 int gcnsa_op_gemm_packed8(void* stream, int64_t n, int32_t f, int32_t c, const gcnsa_packed8* x, const float* g,
                           int64_t ldg, float* dw, int64_t lddw, int32_t accumulate, void* workspace,
@@ -696,8 +697,12 @@ size_t gcnsa_op_gemm_packed8_workspace(int64_t n, int32_t f, int32_t c);
  * masked rows (n without a mask); with another number the loss comes out as NaN.
  * n_train = 0: loss 0, zero gradients.  Labels of masked rows lie in [0, c); one
  * that does not makes the loss NaN (nothing is read or written out of place).
- * Rows that do not count (mask 0) may hold anything in h and y: their dh is 0 and
- * nothing else depends on them.
+ * Rows that do not count (mask 0) may hold anything in h and y: their dh is 0
+ * (w being finite) and nothing else depends on them.  A class whose bias is
+ * -infinity is left out (probability and gradients 0).  What an infinity or a NaN
+ * in w, or in a row of h that counts, enters is NaN, the loss among it (so with a
+ * bias of +infinity), also where
+ * the formula has an infinity or a probability of 0.
  * accumulate applies to dw and db.  d, c >= 1; n, d, c < 2^31 - 2^17, n c < 2^45; workspace: DEVICE,
  * 256-byte aligned, gcnsa_op_linear_ce_workspace(n, d, c) bytes. */
 int gcnsa_op_linear_ce(void* stream, int64_t n, int32_t d, int32_t c, const float* h, int64_t ldh, const float* w,

@@ -175,7 +175,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 constexpr float kLog2e = 1.44269504088896340736f;
 // Two values as three pairs of bf16 terms, the first value in the lower halves.  Every term is what its upper 16 bits say (cut
 // off, not rounded: no finite value becomes an infinity, and a byte permute packs two of them, where cvt.rn.bf16x2 has a
-// fraction of that rate); 8 + 8 + 8 bits are all that a value has.
+// fraction of that rate); 8 + 8 + 8 bits are all that a value has.  An infinity leaves a NaN as its second term: products with
+// one are NaN.  (To keep it would take a test per value, and infinity times a second term of 0 is NaN all the same.)
 __device__ __forceinline__ void split3(float x0, float x1, uint32_t& t0, uint32_t& t1, uint32_t& t2) {
   auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); };
   t0 = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);

@@ -158,3 +158,28 @@ def test_norm_backward_of_equal_values_far_from_zero(f):
                                              scratch=_bytes(gcnsa.op_layer_norm_backward_scratch(n, f)))
                 _within(dx[:, :f], want, bound, f"dx f={f}")
                 assert torch.all(dg == 0)
+
+
+# ------------------------------------------------- infinities in operands ---
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("c", [41, 700])
+def test_values_that_are_not_finite_make_nan_of_what_they_enter(c, bad):
+    """Also an infinity, also where the formula has an infinity or a probability of 0: it has no terms to be cut into."""
+    n, d = 200, 24
+    h, w, y = _rand(1, n, d), _rand(2, d, c), torch.arange(n, device="cuda", dtype=torch.int32) % c
+    one = h.clone()
+    one[17, 3] = bad
+    got = _ce_run(one, w, None, y, None, n)
+    rest = torch.arange(n, device="cuda") != 17
+    assert torch.isnan(got["loss"]) and torch.isnan(got["dh"][17]).all() and torch.isfinite(got["dh"][rest]).all()
+    assert torch.isnan(got["dw"]).all() and torch.isnan(got["db"]).all()
+    w[5, 7] = bad
+    got = _ce_run(h, w, None, y, None, n)
+    assert torch.isnan(got["loss"]) and all(torch.isnan(got[k]).all() for k in ("dh", "dw", "db"))
+    f = 40
+    p, g = gcnsa.Packed8(n, f), _rand(3, n, c)
+    gcnsa.op_pack8(_rand(4, n, f), p)
+    g[100, 6] = bad
+    dw = torch.empty(f, c, device="cuda")
+    gcnsa.op_gemm_packed8(p, g, c, dw, workspace=_bytes(gcnsa.op_gemm_packed8_workspace(n, f, c)))
+    assert torch.isnan(dw[:, 6]).all() and torch.isfinite(dw[:, :6]).all() and torch.isfinite(dw[:, 7:]).all()
