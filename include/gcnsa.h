@@ -651,7 +651,8 @@ typedef struct {
  * checkpoints of x and of y in the same pass; bits: nullable DEVICE [n x ldbits],
  * ldbits >= ceil(f / 32), with relu only: bit j % 32 of word j / 32 of a row says
  * whether the ReLU let value j through.  y may be x (same ld).  1 <= f <=
- * GCNSA_NORM_MAX_F, eps > 0. */
+ * GCNSA_NORM_MAX_F, eps > 0.  Sums are held in 32 bits: a row whose sum passes
+ * 3.4e38 has NaN, one whose squared deviations do has rstd = 0. */
 #define GCNSA_NORM_MAX_F (1 << 24)
 int gcnsa_op_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int64_t ldx, const float* gamma,
                         const float* beta, float eps, int32_t relu, float* y, int64_t ldy, float* mean, float* rstd,
@@ -663,7 +664,8 @@ int gcnsa_op_layer_norm(void* stream, int64_t n, int32_t f, const float* x, int6
  * dx = rstd (u - mean(u) - xh mean(u xh)); dgamma[j] (+)= sum_i g[i, j] xh[i, j] and
  * dbeta[j] (+)= sum_i g[i, j] over the gradients the ReLU let through.  The input
  * is either x or its checkpoint x8 (the other one NULL).  mean, rstd: DEVICE [n],
- * from the forward pass; gamma, beta, dgamma, dbeta nullable; dx may be g or x
+ * from the forward pass (the mean is rounded to 32 bits: xh of a row is off by up
+ * to 2^-24 |mean| rstd, which the forward pass's y is not); gamma, beta, dgamma, dbeta nullable; dx may be g or x
  * (same ld).  scratch: DEVICE, gcnsa_op_layer_norm_backward_scratch(n, f) bytes,
  * not needed (NULL) without dgamma and dbeta.  Sums are added in a fixed order. */
 int gcnsa_op_layer_norm_backward(void* stream, int64_t n, int32_t f, const float* g, int64_t ldg, const float* x,

@@ -243,7 +243,8 @@ __device__ __forceinline__ void load_cols(const float* __restrict__ w, float non
 }
 
 // The mean is corrected by the mean of what is left after subtracting it, and the variance is taken around the corrected
-// one: a column offset of 1e4 next to a spread of 1 then costs no digits, as the differences x - mean are exact.
+// one: y and rstd of a row 1e4 off zero with a spread of 1 then lose no digits, as the differences x - mean are exact.  (The mean is
+// handed to the backward pass in 32 bits, half a unit of it off, and xh is shifted by as much there: 5e-4 in such a row.)
 //
 // A short row is the chain load - two sums across lanes - store: a warp that holds few float4 of a row works on R at a time
 // (200 000 x 100: 66 us with one, 56 with four); two rows share a block's barriers (33 333 x 1 500: 121 and 109; by 4-byte

@@ -160,6 +160,31 @@ def test_norm_backward_of_equal_values_far_from_zero(f):
                 assert torch.all(dg == 0)
 
 
+@pytest.mark.parametrize("f", [5, 41, 128, 602, 1500])
+def test_norm_backward_with_offsets_is_off_by_the_mean_s_rounding(f):
+    """Rows 1e4 off zero with a spread of 1.  The forward pass hands on the mean in 32 bits, half a unit of 1e4 off, and xh of the
+    whole row is shifted by that: the gradient is that of the shifted xh, not closer."""
+    n = 300
+    x = 1e4 + _rand(f, n, f)
+    g = _rand(f + 1, n, f)
+    y, mean, rstd, dx = torch.empty(n, f, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, f, device="cuda")
+    dg = torch.empty(f, device="cuda")
+    gcnsa.op_layer_norm(x, f, y, mean=mean, rstd=rstd)
+    gcnsa.op_layer_norm_backward(g, x, f, dx, mean, rstd, dgamma=dg, scratch=_bytes(gcnsa.op_layer_norm_backward_scratch(n, f)))
+    x, g = x.double(), g.double()
+    m = x.mean(1, keepdim=True)
+    r = 1 / torch.sqrt(((x - m) ** 2).mean(1, keepdim=True) + 1e-5)
+    xh = (x - m) * r
+    c2, g1 = (g * xh).mean(1, keepdim=True), g.abs().mean(1, keepdim=True)
+    want = r * (g - g.mean(1, keepdim=True) - xh * c2)
+    k = max(32, f / 256) + 25
+    shift = U * m.abs() * r + (k + 8) * U               # of xh; the sum of the mean itself has the depth of the rows' deviations
+    size = r * (g.abs() + g1 + xh.abs() * (g * xh).abs().mean(1, keepdim=True))
+    moved = r * (shift * (c2.abs() + xh.abs() * g1) + shift ** 2 * g1)
+    _within(dx, want, 2 * k * U * size + moved, f"dx f={f}")
+    _within(dg, (g * xh).sum(0), (g.abs() * shift).sum(0) + (n + 24 + k) * U * (g * xh).abs().sum(0), "dgamma")
+
+
 # ------------------------------------------------- infinities in operands ---
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("c", [41, 700])
@@ -183,3 +208,19 @@ def test_values_that_are_not_finite_make_nan_of_what_they_enter(c, bad):
     dw = torch.empty(f, c, device="cuda")
     gcnsa.op_gemm_packed8(p, g, c, dw, workspace=_bytes(gcnsa.op_gemm_packed8_workspace(n, f, c)))
     assert torch.isnan(dw[:, 6]).all() and torch.isfinite(dw[:, :6]).all() and torch.isfinite(dw[:, 7:]).all()
+
+
+@pytest.mark.parametrize("f", [9, 100, 1500, 8200])
+def test_norms_of_rows_beyond_fp32_sums(f):
+    """A sum beyond the largest fp32 number is an infinity (the row NaN), squares beyond it make rstd 0 (the row beta); other rows
+    keep their values."""
+    x, beta = _rand(f, 40, f), _rand(f + 1, f)
+    y, rstd = torch.empty(40, f, device="cuda"), torch.empty(40, device="cuda")
+    gcnsa.op_layer_norm(x, f, y, beta=beta, rstd=rstd)
+    far, yf, rf = x.clone(), torch.empty(40, f, device="cuda"), torch.empty(40, device="cuda")
+    far[5], far[6] = 3e38, x[6] * 1e25
+    gcnsa.op_layer_norm(far, f, yf, beta=beta, rstd=rf)
+    assert torch.isnan(yf[5]).all() and torch.isnan(rf[5])
+    assert torch.equal(yf[6], beta) and rf[6] == 0
+    rest = [i for i in range(40) if i not in (5, 6)]
+    assert torch.equal(yf[rest], y[rest]) and torch.equal(rf[rest], rstd[rest])
