@@ -20,8 +20,8 @@
 //
 // A k-block of 32 of a 128 x 128 tile keeps the tensor pipe busy for 768 clocks (12 MMAs) and shared memory for about
 // 1 090 (boxes in 256, both read for the split 256, terms of B out 192, B read by the MMAs 384, at 128 bytes a clock).
-// Counters of the passes over 20 011 x 256 x 10 007 classes: tensor pipe 50-56 % busy, issue slots 64-74 %, ALUs 58-64 %, DRAM at
-// most 26 %; of a weight gradient from a checkpoint (245 000 rows, 256 x 256): 40 %, 74 %, 59 %, 33 %.  Making terms, not
+// Counters of the passes over 20 011 x 256 x 10 007 classes: tensor pipe 50-58 % busy, issue slots 66-74 %, ALUs 60-65 %, DRAM at
+// most 28 %; of a weight gradient from a checkpoint (245 000 rows, 256 x 256): 40 %, 74 %, 58 %, 36 %.  Making terms, not
 // the MMAs, is what these products wait for.
 #pragma once
 #include <cuda.h>

@@ -28,7 +28,7 @@ def scenario():
         bufs = _step_buffers(*args[0].shape, args[4].shape[1], c)
         _step(*args, bufs)
         out["step", c] = [bufs[k] for k in ("loss", "h", "dwo", "dbo", "dgamma", "dbeta", "dw", "dt")]
-    for n, d, c in ((1, 5, 300), (3001, 33, 129), (5000, 40, 1500)):   # the last one in several pieces of tiles
+    for n, d, c in ((1, 5, 300), (3001, 33, 129), (5000, 40, 1500)):
         h, w, y = _rand(n, n, d), _rand(d, d, c) / 8, torch.arange(n, device="cuda", dtype=torch.int32) % c
         for share in (0.0, 0.03, 0.6, 1.0):
             mask = (torch.rand(n, generator=torch.Generator().manual_seed(n)) < share).to(torch.uint8).cuda()

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2012_04930_b200 import gcnsa
-from test_gpu_norm_head import U, _buf, _bytes, _ce_run, _empty, _rand, _within
+from test_gpu_norm_head import U, _buf, _bytes, _ce64, _ce_run, _empty, _rand, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -224,3 +224,22 @@ def test_norms_of_rows_beyond_fp32_sums(f):
     assert torch.equal(yf[6], beta) and rf[6] == 0
     rest = [i for i in range(40) if i not in (5, 6)]
     assert torch.equal(yf[rest], y[rest]) and torch.equal(rf[rest], rstd[rest])
+
+
+@pytest.mark.parametrize("padded,masked", [(True, True), (False, True), (True, False)])
+def test_output_layer_in_several_pieces(padded, masked):
+    """G^T of all classes is beyond what is kept of it at a time (160 MB): dh is added up over pieces of the classes, and
+    weights and biases of every piece have their own columns."""
+    n, d, c = 3001, 21, 30011
+    h, w, bias = torch.relu(_rand(1, n, d)) * 2, _rand(2, d, c) / math.sqrt(d), _rand(3, c)
+    y = (torch.arange(n, device="cuda", dtype=torch.int32) * 7919) % c
+    mask = (_rand(4, n) < 0.9).to(torch.uint8) if masked else None
+    nt = n if mask is None else int(mask.sum())
+    assert nt * c * 4 > 160 * 2 ** 20
+    ref = _ce64(h, w, bias, y, mask, nt)
+    start = (_rand(5, d, c) / 1000, _rand(6, c) / 1000)
+    got = _ce_run(h, w, bias, y, mask, nt, padded, accumulate=1, start=start)
+    for k, add in (("loss", 0), ("dh", 0), ("dw", start[0].double()), ("db", start[1].double())):
+        _within(got[k], ref[k][0] + add, ref[k][1] + 2 * U * (ref[k][0].abs() + abs(add)), k)
+    again = _ce_run(h, w, bias, y, mask, nt, padded, want=("dh",))
+    assert torch.equal(again["dh"], got["dh"]) and torch.equal(again["loss"], got["loss"])
